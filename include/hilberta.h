@@ -339,6 +339,91 @@ int hilberta_forward_fused(const void *q, const void *k, const void *v, void *ou
 int hilberta_forward_host(const void *q, const void *k, const void *v, void *out,
                           hilberta_plan_t *plan, void *stream);
 
+/* ---- operators of the transformer block around the attention -------------------------------------------------
+ *
+ * Calls without a plan: pointers are memory of the current device (which must be compute capability 10.x, else
+ * ERR_ARCH), launches are asynchronous on `stream`, nothing is allocated and nothing synchronises, so they can be
+ * captured into a CUDA graph.  Outputs must not overlap inputs or one another except where a call says so. */
+
+/* Layer norm over the last axis, as in front of a block's projections:
+ *     mean = sum x / cols,   rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps),
+ *     y = (x - mean) * rstd * (weight [+ 1]) + bias.
+ * The paper's transformers modulate the normalised rows by one scale and one shift per sample (adaptive layer
+ * norm, Sec. 4.1's models); that is the same call with one weight row per group of rows.
+ *
+ *   x, y            device pointers, [rows, cols] of `dtype` with row strides stride_x, stride_y (elements;
+ *                   stride_y >= cols).  y may be x itself (same stride).
+ *   weight, bias    device pointers or NULL (1 and 0): row r uses row r / rows_per_group of each, rows stride_w
+ *                   elements apart (two slices of one modulation tensor share it); rows_per_group = 0: one row
+ *                   for all.  unit_offset != 0 adds 1 to the weight.
+ *   mean, rstd      device pointers to [rows] fp32 or NULL: what the backward pass reads.
+ *   rows >= 0; 1 <= cols <= 16384 (more: ERR_UNSUPPORTED); any stride and alignment (16-byte aligned rows are
+ *   faster); eps >= 0.
+ *   dtype           HILBERTA_BF16 or HILBERTA_FP32; weight_dtype the same or HILBERTA_FP32.  Sums are fp32.
+ * Errors: ERR_INVALID, ERR_UNSUPPORTED, ERR_ARCH, ERR_CUDA. */
+int hilberta_layer_norm(const void *x, const void *weight, const void *bias, void *y, float *mean, float *rstd,
+                        int64_t rows, int cols, int64_t rows_per_group, int64_t stride_x, int64_t stride_y,
+                        int64_t stride_w, int dtype, int weight_dtype, int unit_offset, float eps, void *stream);
+
+/* Gradients of sum(y * dy):  with n = (x - mean) * rstd and g = dy * (weight [+ 1]),
+ *     dx = rstd * (g - sum g / cols - n * sum(g n) / cols),   dweight = sum_rows dy n,   dbias = sum_rows dy,
+ * the latter two over the rows of each group (rows stride_dw elements apart, weight_dtype).
+ *   dx, dweight, dbias   any of them may be NULL, not all three.  dx may be dy or x itself (same stride).
+ *   mean, rstd           as hilberta_layer_norm wrote them.
+ *   workspace            hilberta_layer_norm_workspace() bytes of device memory, 16-byte aligned, which the call
+ *                        overwrites (NULL where that says 0, or without dweight and dbias); calls that may overlap on the device
+ *                        need one each.  ERR_BUFFER if it is too small.
+ * Sums over rows are taken in a fixed order: the same call gives the same bits.  At most 65535 groups.  rows = 0
+ * writes zeros to the one row of dweight and dbias. */
+int hilberta_layer_norm_backward(const void *dy, const void *x, const void *weight, const float *mean, const float *rstd,
+                                 void *dx, void *dweight, void *dbias, void *workspace, size_t workspace_bytes, int64_t rows,
+                                 int cols, int64_t rows_per_group, int64_t stride_dy, int64_t stride_x, int64_t stride_dx,
+                                 int64_t stride_w, int64_t stride_dw, int dtype, int weight_dtype, int unit_offset, void *stream);
+size_t hilberta_layer_norm_workspace(int64_t rows, int cols, int64_t rows_per_group);
+
+/* Rotary positions, the step between the QKV projection and Algorithm 1 (Sec. 3.3 anchors them in the shared
+ * region).  Pair j of every head turns by t = position[axis[j]] * inv_freq[j]:
+ *     a' = factor * (a cos t - b sin t),   b' = factor * (a sin t + b cos t),
+ * where (a, b) are elements (j, j + pairs), or (2 j, 2 j + 1) with interleaved != 0; elements from 2 * pairs on are
+ * copied.  Angles are exact for every 32-bit position (64-bit fractions of a turn).
+ *
+ *   x, out        device pointers, [batch, heads, S, head_dim] of `dtype` (HILBERTA_BF16 or HILBERTA_FP32) with the
+ *                 element strides strides[0..2] (batch, head, token) of x and strides[3..5] of out, none negative.
+ *                 out may be x itself (same strides, no plan).  A packed [tokens, heads, head_dim] tensor is batch 1.
+ *   positions     device pointer to int32 [batch, S, axes] (position_stride_b positions between batch items; 0: one
+ *                 table for all), in the token order of x; NULL: a token's index in x (axes = 1).
+ *   inv_freq      HOST pointer, `pairs` doubles in radians per position; axis: HOST pointer, `pairs` int32 below
+ *                 `axes`, or NULL (all 0).  Both are read before the call returns.
+ *   plan          NULL, or a plan with S tokens: x is in ORIGINAL order and out in PHYSICAL order (row p of out is
+ *                 token phys2orig[p]; the entry gather of Sec. 3.4 fused in).
+ *   1 <= pairs <= head_dim / 2, head_dim <= 256, axes <= 16, batch * S < 2^31.
+ * Errors: ERR_INVALID, ERR_UNSUPPORTED, ERR_ARCH, ERR_CUDA. */
+int hilberta_rotary(const void *x, void *out, const int32_t *positions, const double *inv_freq, const int32_t *axis,
+                    int pairs, int axes, int interleaved, double factor, const hilberta_plan_t *plan, int batch, int heads,
+                    int S, int head_dim, int dtype, const int64_t *strides, int64_t position_stride_b, void *stream);
+
+/* The gradient: the same with the angles turned back.  With a plan, dout is in PHYSICAL and dx in ORIGINAL order
+ * (the exit gather fused in); positions stay in the ORIGINAL order. */
+int hilberta_rotary_backward(const void *dout, void *dx, const int32_t *positions, const double *inv_freq, const int32_t *axis,
+                             int pairs, int axes, int interleaved, double factor, const hilberta_plan_t *plan, int batch,
+                             int heads, int S, int head_dim, int dtype, const int64_t *strides, int64_t position_stride_b,
+                             void *stream);
+
+/* inv_freq[j] = base^(-j / pairs) on the host, scaled for contexts `scale` times as long as the trained one:
+ *   PLAIN    as it is;
+ *   LINEAR   / scale (positions interpolated);
+ *   BASE     with base * scale^(pairs / (pairs - 1)): the lowest frequency / scale, the highest kept;
+ *   BANDS    frequencies that make fewer than `slow` turns over `context` (the trained context) / scale, those that
+ *            make more than `fast` kept, a linear ramp in the number of turns between; *factor (if not NULL) receives
+ *            1 + 0.1 ln scale, and 1 with the others.
+ * Errors: ERR_INVALID. */
+#define HILBERTA_ROTARY_PLAIN 0
+#define HILBERTA_ROTARY_LINEAR 1
+#define HILBERTA_ROTARY_BASE 2
+#define HILBERTA_ROTARY_BANDS 3
+int hilberta_rotary_frequencies(double *inv_freq, int pairs, double base, int scaling, double scale, double context, double slow,
+                                double fast, double *factor);
+
 /* After a forward on `stream` has completed: 0, or ERR_TIMEOUT if a bounded wait
  * inside the kernel gave up (the output is then undefined).  Synchronises the
  * device.  Clears the flag. */

@@ -31,11 +31,15 @@ SYMBOLS = (
     "hilberta_backward_static", "hilberta_permute",
     "hilberta_unpermute",
     "hilberta_forward_host",
+    "hilberta_layer_norm", "hilberta_layer_norm_backward", "hilberta_layer_norm_workspace",
+    "hilberta_rotary", "hilberta_rotary_backward", "hilberta_rotary_frequencies",
     "hilberta_check_work_list", "hilberta_check_overlap", "hilberta_schedule_units", "hilberta_cut_schedule",
     "hilberta_check_shares",
     "hilberta_plan_status", "hilberta_selftest_timeout", "hilberta_launch_count", "hilberta_status_string", "hilberta_version",
     "hilberta_last_cuda_error",
 )
+
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_BANDS = range(4)
 
 _lib = None
 
@@ -92,6 +96,19 @@ def lib():
         f = getattr(L, name)
         f.argtypes = [vp, vp, vp, i32, i32, i32, vp]
         f.restype = i32
+    L.hilberta_layer_norm.argtypes = [vp] * 6 + [i64, i32] + [i64] * 4 + [i32] * 3 + [f32, vp]
+    L.hilberta_layer_norm.restype = i32
+    L.hilberta_layer_norm_backward.argtypes = [vp] * 9 + [sz, i64, i32] + [i64] * 6 + [i32] * 3 + [vp]
+    L.hilberta_layer_norm_backward.restype = i32
+    L.hilberta_layer_norm_workspace.argtypes = [i64, i32, i64]
+    L.hilberta_layer_norm_workspace.restype = sz
+    f64 = ctypes.c_double
+    for name in ("hilberta_rotary", "hilberta_rotary_backward"):
+        f = getattr(L, name)
+        f.argtypes = [vp] * 5 + [i32] * 3 + [f64, vp] + [i32] * 5 + [vp, i64, vp]
+        f.restype = i32
+    L.hilberta_rotary_frequencies.argtypes = [vp, i32, f64, i32, f64, f64, f64, f64, vp]
+    L.hilberta_rotary_frequencies.restype = i32
     L.hilberta_check_work_list.argtypes = [vp, i32, i32, i32, i32]
     L.hilberta_check_work_list.restype = i32
     i64, u64 = ctypes.c_int64, ctypes.c_uint64
@@ -364,6 +381,193 @@ def hilberta_permute(src, dst, plan: Plan, stream=None):
 
 def hilberta_unpermute(src, dst, plan: Plan, stream=None):
     return plan.unpermute(src, dst, stream)
+
+
+# ---- operators of the block around the attention ---------------------------------------------------------------
+
+def _here(*tensors):
+    """The tensors live on the current CUDA device (the library launches there)."""
+    device = _current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"tensor on {t.device}, the current device is cuda:{device}")
+
+
+def _current_device() -> int:
+    global _current_device
+    import torch
+    device = int(torch.cuda.current_device())   # initialises torch's side of CUDA if need be
+    _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return device
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _rows(t, name):
+    """(rows, row stride) of a [..., cols] tensor whose leading axes are one."""
+    if t.dim() < 1 or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name}: the last axis has to be contiguous")
+    if t.is_contiguous():
+        return t.numel() // max(t.shape[-1], 1), t.shape[-1]
+    rows, stride = 1, 0
+    for n, st in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n == 1:
+            continue
+        if rows > 1 and st != rows * stride:
+            raise ValueError(f"{name}: rows have to be evenly spaced")
+        if rows == 1:
+            stride = st
+        rows *= n
+    return rows, max(stride, t.shape[-1])
+
+
+def _norm_weights(x, tensors):
+    """(rows per group, row stride, dtype code) of the weight-like tensors [cols] or [groups, cols]."""
+    given = [t for t in tensors if t is not None]
+    if not given:
+        return 0, 0, _dtype_code(x)
+    w = given[0]
+    cols = x.shape[-1]
+    for t in given:
+        if t.shape != w.shape or t.dtype != w.dtype or t.shape[-1] != cols or (cols > 1 and t.stride(-1) != 1):
+            raise ValueError("weight, bias and their gradients: one shape and dtype, [cols] or [groups, cols]")
+    if w.dim() == 1:
+        return 0, cols, _dtype_code(w)
+    if w.dim() != 2 or x.dim() < 2 or w.shape[0] != x.shape[0]:
+        raise ValueError("weights of a group of rows are [x.shape[0], cols]")
+    groups = w.shape[0]
+    per = x.numel() // (cols * groups) if groups and cols else 0
+    return (0 if groups == 1 else per), w.stride(0), _dtype_code(w)
+
+
+def _same_stride(a, b, what):
+    if a is not None and b is not None and a.dim() == 2 and a.shape[0] > 1 and a.stride(0) != b.stride(0):
+        raise ValueError(f"{what} have to share a row stride")
+
+
+def layer_norm(x, weight, bias, y, mean=None, rstd=None, eps=1e-6, unit_offset=False, stream=None):
+    """y = (x - mean) * rstd * (weight [+ 1]) + bias over the last axis of x [..., cols].
+
+    weight, bias: None, [cols], or [x.shape[0], cols] (one row per sample).  mean, rstd: None or fp32 [...] to be
+    written for layer_norm_backward.  y may be x."""
+    rows, sx = _rows(x, "x")
+    _, sy = _rows(y, "y")
+    if y.shape != x.shape or y.dtype != x.dtype:
+        raise ValueError("x and y must match")
+    _statistics(x, mean, rstd)
+    per, sw, wcode = _norm_weights(x, (weight, bias))
+    _same_stride(weight, bias, "weight and bias")
+    _here(x, y, weight, bias, mean, rstd)
+    _check(lib().hilberta_layer_norm(x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), _ptr(mean), _ptr(rstd), rows,
+                                     x.shape[-1], per, sx, sy, sw, _dtype_code(x), wcode, int(bool(unit_offset)), eps,
+                                     _stream_ptr(stream)), "hilberta_layer_norm")
+    return y, mean, rstd
+
+
+def _statistics(x, *tensors):
+    for t in tensors:
+        if t is not None and (t.shape != x.shape[:-1] or not t.is_contiguous() or _dtype_code(t) != FP32):
+            raise ValueError("mean and rstd: contiguous fp32 of x's shape without the last axis")
+
+
+def layer_norm_workspace(x, weight=None) -> int:
+    """Bytes of workspace that layer_norm_backward needs for x and weight (or one of their gradients)."""
+    per = _norm_weights(x, (weight,))[0]
+    return int(lib().hilberta_layer_norm_workspace(x.numel() // max(x.shape[-1], 1), x.shape[-1], per))
+
+
+def layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, unit_offset=False, workspace=None, stream=None):
+    """Gradients of layer_norm into dx, dweight, dbias (any may be None, not all).  workspace: None (taken from torch's
+    allocator on the current stream) or a uint8 tensor of layer_norm_workspace() bytes."""
+    import torch
+    rows, sx = _rows(x, "x")
+    _, sdy = _rows(dy, "dy")
+    sdx = 0
+    if dx is not None:
+        sdx = _rows(dx, "dx")[1]
+    for t in (dy, dx):
+        if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
+            raise ValueError("dy, x and dx must match")
+    if mean is None or rstd is None:
+        raise ValueError("mean and rstd of the forward pass are needed")
+    _statistics(x, mean, rstd)
+    per, _, wcode = _norm_weights(x, (weight, dweight, dbias))
+    sw = weight.stride(0) if weight is not None and weight.dim() == 2 else 0
+    g = dweight if dweight is not None else dbias
+    sdw = g.stride(0) if g is not None and g.dim() == 2 else 0
+    _same_stride(dweight, dbias, "dweight and dbias")
+    _here(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace)
+    L = lib()
+    if workspace is None and g is not None:
+        n = int(L.hilberta_layer_norm_workspace(rows, x.shape[-1], per))
+        if n:
+            if stream is None:
+                workspace = torch.empty(n, dtype=torch.uint8, device=x.device)
+            else:
+                with torch.cuda.stream(stream):
+                    workspace = torch.empty(n, dtype=torch.uint8, device=x.device)
+    _check(L.hilberta_layer_norm_backward(dy.data_ptr(), x.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(), _ptr(dx),
+                                          _ptr(dweight), _ptr(dbias), _ptr(workspace),
+                                          0 if workspace is None else workspace.numel() * workspace.element_size(), rows,
+                                          x.shape[-1], per, sdy, sx, sdx, sw, sdw, _dtype_code(x), wcode,
+                                          int(bool(unit_offset)), _stream_ptr(stream)), "hilberta_layer_norm_backward")
+    return dx, dweight, dbias
+
+
+def rotary_frequencies(pairs, base=10000.0, scaling=ROTARY_PLAIN, scale=1.0, context=0.0, slow=1.0, fast=32.0):
+    """(inv_freq, factor): `pairs` fp64 frequencies on the CPU and the factor that goes with them (host only)."""
+    import torch
+    f, factor = torch.empty(int(pairs), dtype=torch.float64), ctypes.c_double(1.0)
+    _check(lib().hilberta_rotary_frequencies(f.data_ptr(), int(pairs), float(base), int(scaling), float(scale), float(context),
+                                             float(slow), float(fast), ctypes.addressof(factor)), "hilberta_rotary_frequencies")
+    return f, factor.value
+
+
+def _rotary(fn, name, x, out, inv_freq, positions, axis, interleaved, factor, plan, stream):
+    import torch
+    if x.dim() != 4 or out.shape != x.shape or out.dtype != x.dtype:
+        raise ValueError("x and out: [batch, heads, S, head_dim], one shape and dtype")
+    B, H, S, D = x.shape
+    if D > 1 and (x.stride(3) != 1 or out.stride(3) != 1):
+        raise ValueError("the head_dim axis has to be contiguous")
+    if inv_freq.dtype != torch.float64 or inv_freq.is_cuda or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+        raise ValueError("inv_freq: contiguous fp64 [pairs] on the CPU")
+    axes, pos_stride = 1, 0
+    if axis is not None and (axis.dtype != torch.int32 or axis.is_cuda or axis.shape != inv_freq.shape or not axis.is_contiguous()):
+        raise ValueError("axis: contiguous int32 [pairs] on the CPU")
+    if positions is not None:
+        if positions.dtype != torch.int32 or not positions.is_contiguous():
+            raise ValueError("positions: contiguous int32")
+        shape = tuple(positions.shape)
+        if axis is not None:
+            if not shape:
+                raise ValueError("positions: [S, axes] or [batch, S, axes]")
+            axes, shape = shape[-1], shape[:-1]
+        if shape == (B, S):
+            pos_stride = S
+        elif shape != (S,):
+            raise ValueError("positions: [S] or [batch, S], with an axis for each position axis if `axis` is given")
+    _here(x, out, positions)
+    strides = (ctypes.c_int64 * 6)(x.stride(0), x.stride(1), x.stride(2), out.stride(0), out.stride(1), out.stride(2))
+    _check(fn(x.data_ptr(), out.data_ptr(), _ptr(positions), inv_freq.data_ptr(), _ptr(axis), inv_freq.numel(), axes,
+              int(bool(interleaved)), factor, None if plan is None else plan._h, B, H, S, D, _dtype_code(x), strides, pos_stride,
+              _stream_ptr(stream)), name)
+    return out
+
+
+def rotary(x, out, inv_freq, positions=None, axis=None, interleaved=False, factor=1.0, plan=None, stream=None):
+    """Rotary positions on x [batch, heads, S, head_dim] into out (x itself for in place).  positions: int32 [S] or
+    [batch, S], with a last axis of position axes if `axis` (int32 [pairs] on the CPU) is given; None: the token's index.
+    plan: x in ORIGINAL order, out in PHYSICAL order."""
+    return _rotary(lib().hilberta_rotary, "hilberta_rotary", x, out, inv_freq, positions, axis, interleaved, factor, plan, stream)
+
+
+def rotary_backward(dout, dx, inv_freq, positions=None, axis=None, interleaved=False, factor=1.0, plan=None, stream=None):
+    """The gradient of rotary(): dx from dout; with a plan, dout in PHYSICAL and dx in ORIGINAL order."""
+    return _rotary(lib().hilberta_rotary_backward, "hilberta_rotary_backward", dout, dx, inv_freq, positions, axis, interleaved,
+                   factor, plan, stream)
 
 
 def trim() -> int:

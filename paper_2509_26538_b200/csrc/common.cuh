@@ -5,6 +5,7 @@
 #include <string.h>
 
 #include <atomic>
+#include <mutex>
 #include <new>
 #include <vector>
 
@@ -210,6 +211,13 @@ namespace hilberta {
 __device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// Gathers of up to this many bytes may overlap the kernel before them.  They run for a few microseconds each,
+// and launch latency is part of that; large ones that run into one another leave the forward after them less of
+// K and V in L2.  Three gathers and a forward, overlapping / plain, by the bytes of one gather (B200, us): 2 MB 21.6 /
+// 27.8, 5 MB 31.3 / 32.9, 13 MB 89 / 97, 28 MB 158 / 160, 33 MB 182.6 / 182.3, 47 MB 257.8 / 257.2, 52 MB (e4m3) 438 / 441,
+// 52 MB (head dim 64) 421 / 423, 70 MB 374 / 369, 104 MB 625 / 612, 415 MB 4190 / 4120.
+constexpr size_t kOverlapBytes = 32u << 20;
+
 template <class... Params, class... Args>
 cudaError_t launch_overlapping(void (*kernel)(Params...), dim3 grid, unsigned block, size_t smem, unsigned cluster,
                                cudaStream_t stream, bool overlap, const Args &...args) {
@@ -228,6 +236,29 @@ cudaError_t launch_overlapping(void (*kernel)(Params...), dim3 grid, unsigned bl
     config.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&config, kernel, Params(args)...);
 }
+
+// SMs of a device of compute capability 10.x, 0 for any other.
+inline int sm100_count(int device) {
+    static std::mutex mutex;
+    static int count[64] = {};
+    if (device < 0 || device >= 64) return 0;
+    std::lock_guard<std::mutex> lock(mutex);
+    int major = 0;
+    if (!count[device] && cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, device) == cudaSuccess && major == 10)
+        cudaDeviceGetAttribute(&count[device], cudaDevAttrMultiProcessorCount, device);
+    return count[device];
+}
+
+// n / d for n < 2^31 by a multiplication (Granlund and Montgomery, 1994): with s = ceil(log2 d),
+// q = (mulhi(n, floor(2^32 (2^s - d) / d) + 1) + n) >> s.
+struct Divider {
+    unsigned d, mul, shift;
+    explicit Divider(int div)
+        : d((unsigned)div), mul(0), shift(div > 1 ? 32 - __builtin_clz((unsigned)div - 1) : 0) {
+        mul = (unsigned)(((((unsigned long long)1 << shift) - d) << 32) / d + 1);
+    }
+    __device__ __forceinline__ unsigned quotient(unsigned n) const { return (__umulhi(n, mul) + n) >> shift; }
+};
 
 // out_map: nullptr = write rows in physical order; else out_map[p] is the row of `out`
 // that physical row p goes to (the exit gather fused into the epilogue).

@@ -9,23 +9,6 @@ namespace hilberta {
 
 constexpr int kGatherThreads = 256;
 constexpr int kGatherUnroll = 4;
-// Gathers of up to this many bytes may overlap the kernel before them.  They run for a few microseconds each,
-// and launch latency is part of that; large ones that run into one another leave the forward after them less of
-// K and V in L2.  Three gathers and a forward, overlapping / plain, by the bytes of one gather (B200, us): 2 MB 21.6 /
-// 27.8, 5 MB 31.3 / 32.9, 13 MB 89 / 97, 28 MB 158 / 160, 33 MB 182.6 / 182.3, 47 MB 257.8 / 257.2, 52 MB (e4m3) 438 / 441,
-// 52 MB (head dim 64) 421 / 423, 70 MB 374 / 369, 104 MB 625 / 612, 415 MB 4190 / 4120.
-constexpr size_t kOverlapBytes = 32u << 20;
-
-// n / d for n < 2^31 by a multiplication (Granlund and Montgomery, 1994): with s = ceil(log2 d),
-// q = (mulhi(n, floor(2^32 (2^s - d) / d) + 1) + n) >> s.
-struct Divider {
-    unsigned d, mul, shift;
-    explicit Divider(int div)
-        : d((unsigned)div), mul(0), shift(div > 1 ? 32 - __builtin_clz((unsigned)div - 1) : 0) {
-        mul = (unsigned)(((((unsigned long long)1 << shift) - d) << 32) / d + 1);
-    }
-    __device__ __forceinline__ unsigned quotient(unsigned n) const { return (__umulhi(n, mul) + n) >> shift; }
-};
 
 // dst[b, r, :] = src[b, index[r], :]; a row is vecs.d 16-byte vectors, a batch item rows.d rows.  Bound by HBM, and below
 // some 30 MB by its chain of launch, index load, vector load and store.  A block copies kGatherThreads * kGatherUnroll
