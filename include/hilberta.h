@@ -424,6 +424,30 @@ int hilberta_rotary_backward(const void *dout, void *dx, const int32_t *position
 int hilberta_rotary_frequencies(double *inv_freq, int pairs, double base, int scaling, double scale, double context, double slow,
                                 double fast, double *factor);
 
+/* Dense attention within each of n_seq sequences packed one after the other -- the prompts of a batch in a text
+ * encoder, images of several sizes -- in one launch: token t of sequence i is row cu_seqlens[i] + t, and head h
+ * reads key head h / (heads / kv_heads).  causal != 0: token t sees the tokens 0 .. t of its sequence, else all of them.
+ *     out = softmax(scale * q k^T) v,   lse = log sum exp(scale * <q, k>).
+ *
+ *   q, out        device pointers, [total, heads, head_dim] bf16; k, v: [total, kv_heads, head_dim].  strides:
+ *                 element strides (token, head) of q, k, v, out in turn, positive multiples of 8; 16-byte aligned
+ *                 pointers.  They may be slices of one projection's output.
+ *   lse           device pointer to [heads, total] fp32, or NULL.
+ *   cu_seqlens    DEVICE pointer to n_seq + 1 ascending int32, from >= 0 to <= total.  Sequences may be empty.  Rows
+ *                 outside all sequences are neither read into a result nor written, whatever they hold.  Values that
+ *                 are not ascending or leave [0, total] give undefined results and no access out of range.
+ *   kv_heads divides heads; head_dim 64 or 128; dtype HILBERTA_BF16 (others: ERR_UNSUPPORTED); n_seq <= 65536.
+ *   scale         <= 0 selects 1 / sqrt(head_dim).
+ *   values        those of one sequence must be finite for it; other sequences do not matter to it.
+ * Errors: ERR_INVALID, ERR_UNSUPPORTED, ERR_ARCH, ERR_CUDA. */
+int hilberta_packed_forward(const void *q, const void *k, const void *v, void *out, float *lse, const int32_t *cu_seqlens,
+                            int n_seq, int total, int heads, int kv_heads, int head_dim, int dtype, const int64_t *strides,
+                            int causal, float scale, void *stream);
+
+/* 0, or ERR_TIMEOUT if a bounded wait inside a packed attention kernel on the current device has given up since the
+ * last call (that kernel's results are undefined).  Synchronises the device.  Clears the flag. */
+int hilberta_packed_status(void);
+
 /* After a forward on `stream` has completed: 0, or ERR_TIMEOUT if a bounded wait
  * inside the kernel gave up (the output is then undefined).  Synchronises the
  * device.  Clears the flag. */

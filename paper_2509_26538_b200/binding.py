@@ -33,6 +33,7 @@ SYMBOLS = (
     "hilberta_forward_host",
     "hilberta_layer_norm", "hilberta_layer_norm_backward", "hilberta_layer_norm_workspace",
     "hilberta_rotary", "hilberta_rotary_backward", "hilberta_rotary_frequencies",
+    "hilberta_packed_forward", "hilberta_packed_status",
     "hilberta_check_work_list", "hilberta_check_overlap", "hilberta_schedule_units", "hilberta_cut_schedule",
     "hilberta_check_shares",
     "hilberta_plan_status", "hilberta_selftest_timeout", "hilberta_launch_count", "hilberta_status_string", "hilberta_version",
@@ -109,6 +110,10 @@ def lib():
         f.restype = i32
     L.hilberta_rotary_frequencies.argtypes = [vp, i32, f64, i32, f64, f64, f64, f64, vp]
     L.hilberta_rotary_frequencies.restype = i32
+    L.hilberta_packed_forward.argtypes = [vp] * 6 + [i32] * 6 + [vp, i32, f32, vp]
+    L.hilberta_packed_forward.restype = i32
+    L.hilberta_packed_status.argtypes = []
+    L.hilberta_packed_status.restype = i32
     L.hilberta_check_work_list.argtypes = [vp, i32, i32, i32, i32]
     L.hilberta_check_work_list.restype = i32
     i64, u64 = ctypes.c_int64, ctypes.c_uint64
@@ -568,6 +573,55 @@ def rotary_backward(dout, dx, inv_freq, positions=None, axis=None, interleaved=F
     """The gradient of rotary(): dx from dout; with a plan, dout in PHYSICAL and dx in ORIGINAL order."""
     return _rotary(lib().hilberta_rotary_backward, "hilberta_rotary_backward", dout, dx, inv_freq, positions, axis, interleaved,
                    factor, plan, stream)
+
+
+def _packed_shapes(q, k, v, like_q, like_k, lse, cu_seqlens):
+    """(total, heads, kv_heads, head_dim) of packed tensors [total, heads, head_dim]; checks the others against them."""
+    import torch
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("packed tensors are [total, heads, head_dim]")
+    T, H, D = q.shape
+    Hk = k.shape[1]
+    for ts, shape in (((q,) + like_q, (T, H, D)), ((k, v) + like_k, (T, Hk, D))):
+        for t in ts:
+            if t.shape != shape or t.dtype != q.dtype:
+                raise ValueError("packed tensors must match: [total, heads, head_dim] and [total, kv_heads, head_dim], one dtype")
+            if D > 1 and t.stride(2) != 1:
+                raise ValueError("the head_dim axis has to be contiguous")
+    if lse is not None and (lse.shape != (H, T) or not lse.is_contiguous() or lse.dtype != torch.float32):
+        raise ValueError("lse: contiguous fp32 [heads, total]")
+    if cu_seqlens.dtype != torch.int32 or cu_seqlens.dim() != 1 or not cu_seqlens.is_contiguous() or cu_seqlens.numel() < 1:
+        raise ValueError("cu_seqlens: contiguous int32 [sequences + 1]")
+    _here(q, k, v, lse, cu_seqlens, *like_q, *like_k)
+    return T, H, Hk, D
+
+
+def _packed_strides(*tensors):
+    """(token, head) strides of each; an axis of one element has any."""
+    out = []
+    for t in tensors:
+        st, sh = t.stride(0), t.stride(1)
+        D = t.shape[2]
+        if t.shape[1] == 1:
+            sh = (D + 7) // 8 * 8
+        if t.shape[0] <= 1:
+            st = max(t.shape[1], 1) * max(sh, 1)
+        out += [st, sh]
+    return (ctypes.c_int64 * len(out))(*out)
+
+
+def packed_forward(q, k, v, out, cu_seqlens, lse=None, causal=True, scale=0.0, stream=None):
+    """Attention within each of the sequences packed along the first axis: q, out [total, heads, head_dim], k, v
+    [total, kv_heads, head_dim] bf16; cu_seqlens int32 [sequences + 1] on the device; lse None or fp32 [heads, total]."""
+    T, H, Hk, D = _packed_shapes(q, k, v, (out,), (), lse, cu_seqlens)
+    _check(lib().hilberta_packed_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse), cu_seqlens.data_ptr(),
+                                         cu_seqlens.numel() - 1, T, H, Hk, D, _dtype_code(q), _packed_strides(q, k, v, out),
+                                         int(bool(causal)), scale, _stream_ptr(stream)), "hilberta_packed_forward")
+    return out, lse
+
+
+def packed_status() -> int:
+    return int(lib().hilberta_packed_status())
 
 
 def trim() -> int:
