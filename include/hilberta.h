@@ -444,6 +444,20 @@ int hilberta_packed_forward(const void *q, const void *k, const void *v, void *o
                             int n_seq, int total, int heads, int kv_heads, int head_dim, int dtype, const int64_t *strides,
                             int causal, float scale, void *stream);
 
+/* Gradients of sum(out * dout):
+ *     P = exp(scale * q k^T - lse),  dP = dout v^T,  dS = P * (dP - sum_d dout * out),
+ *     dq = scale * dS k,   dk = scale * dS^T q,   dv = P^T dout,   dk and dv summed over the heads of a group.
+ *   out, lse      what hilberta_packed_forward wrote for these q, k, v.
+ *   strides       (token, head) of dout, q, k, v, out, dq, dk, dv in turn.
+ *   workspace     hilberta_packed_workspace(total, heads) bytes of device memory, 16-byte aligned, which the call
+ *                 overwrites; calls that may overlap on the device need one each.  ERR_BUFFER if it is too small.
+ * Every sum is taken in a fixed order: the same call gives the same bits. */
+int hilberta_packed_backward(const void *dout, const void *q, const void *k, const void *v, const void *out, const float *lse,
+                             void *dq, void *dk, void *dv, void *workspace, size_t workspace_bytes, const int32_t *cu_seqlens,
+                             int n_seq, int total, int heads, int kv_heads, int head_dim, int dtype, const int64_t *strides,
+                             int causal, float scale, void *stream);
+size_t hilberta_packed_workspace(int total, int heads);
+
 /* 0, or ERR_TIMEOUT if a bounded wait inside a packed attention kernel on the current device has given up since the
  * last call (that kernel's results are undefined).  Synchronises the device.  Clears the flag. */
 int hilberta_packed_status(void);

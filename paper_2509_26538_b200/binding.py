@@ -33,7 +33,7 @@ SYMBOLS = (
     "hilberta_forward_host",
     "hilberta_layer_norm", "hilberta_layer_norm_backward", "hilberta_layer_norm_workspace",
     "hilberta_rotary", "hilberta_rotary_backward", "hilberta_rotary_frequencies",
-    "hilberta_packed_forward", "hilberta_packed_status",
+    "hilberta_packed_forward", "hilberta_packed_backward", "hilberta_packed_workspace", "hilberta_packed_status",
     "hilberta_check_work_list", "hilberta_check_overlap", "hilberta_schedule_units", "hilberta_cut_schedule",
     "hilberta_check_shares",
     "hilberta_plan_status", "hilberta_selftest_timeout", "hilberta_launch_count", "hilberta_status_string", "hilberta_version",
@@ -112,6 +112,10 @@ def lib():
     L.hilberta_rotary_frequencies.restype = i32
     L.hilberta_packed_forward.argtypes = [vp] * 6 + [i32] * 6 + [vp, i32, f32, vp]
     L.hilberta_packed_forward.restype = i32
+    L.hilberta_packed_backward.argtypes = [vp] * 10 + [sz, vp] + [i32] * 6 + [vp, i32, f32, vp]
+    L.hilberta_packed_backward.restype = i32
+    L.hilberta_packed_workspace.argtypes = [i32, i32]
+    L.hilberta_packed_workspace.restype = sz
     L.hilberta_packed_status.argtypes = []
     L.hilberta_packed_status.restype = i32
     L.hilberta_check_work_list.argtypes = [vp, i32, i32, i32, i32]
@@ -406,6 +410,15 @@ def _current_device() -> int:
     return device
 
 
+def _scratch(n, like, stream):
+    """n bytes of torch's memory that belong to the stream of the call, so that they are reused in its order."""
+    import torch
+    if stream is None:
+        return torch.empty(n, dtype=torch.uint8, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(n, dtype=torch.uint8, device=like.device)
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -485,8 +498,7 @@ def layer_norm_workspace(x, weight=None) -> int:
 
 def layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, unit_offset=False, workspace=None, stream=None):
     """Gradients of layer_norm into dx, dweight, dbias (any may be None, not all).  workspace: None (taken from torch's
-    allocator on the current stream) or a uint8 tensor of layer_norm_workspace() bytes."""
-    import torch
+    allocator) or a uint8 tensor of layer_norm_workspace() bytes."""
     rows, sx = _rows(x, "x")
     _, sdy = _rows(dy, "dy")
     sdx = 0
@@ -508,11 +520,7 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, unit_offs
     if workspace is None and g is not None:
         n = int(L.hilberta_layer_norm_workspace(rows, x.shape[-1], per))
         if n:
-            if stream is None:
-                workspace = torch.empty(n, dtype=torch.uint8, device=x.device)
-            else:
-                with torch.cuda.stream(stream):
-                    workspace = torch.empty(n, dtype=torch.uint8, device=x.device)
+            workspace = _scratch(n, x, stream)
     _check(L.hilberta_layer_norm_backward(dy.data_ptr(), x.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(), _ptr(dx),
                                           _ptr(dweight), _ptr(dbias), _ptr(workspace),
                                           0 if workspace is None else workspace.numel() * workspace.element_size(), rows,
@@ -618,6 +626,29 @@ def packed_forward(q, k, v, out, cu_seqlens, lse=None, causal=True, scale=0.0, s
                                          cu_seqlens.numel() - 1, T, H, Hk, D, _dtype_code(q), _packed_strides(q, k, v, out),
                                          int(bool(causal)), scale, _stream_ptr(stream)), "hilberta_packed_forward")
     return out, lse
+
+
+def packed_workspace(total, heads) -> int:
+    """Bytes of workspace that packed_backward needs."""
+    return int(lib().hilberta_packed_workspace(int(total), int(heads)))
+
+
+def packed_backward(dout, q, k, v, out, lse, dq, dk, dv, cu_seqlens, causal=True, scale=0.0, workspace=None, stream=None):
+    """Gradients of packed_forward into dq, dk, dv, from dout and the forward's inputs, output and lse.  workspace: None
+    (taken from torch's allocator) or a uint8 tensor of packed_workspace() bytes."""
+    if lse is None:
+        raise ValueError("lse of the forward pass is needed")
+    T, H, Hk, D = _packed_shapes(q, k, v, (dout, out, dq), (dk, dv), lse, cu_seqlens)
+    L = lib()
+    if workspace is None:
+        workspace = _scratch(int(L.hilberta_packed_workspace(T, H)), q, stream)
+    _here(workspace)
+    _check(L.hilberta_packed_backward(dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
+                                      dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), workspace.data_ptr(),
+                                      workspace.numel() * workspace.element_size(), cu_seqlens.data_ptr(), cu_seqlens.numel() - 1,
+                                      T, H, Hk, D, _dtype_code(q), _packed_strides(dout, q, k, v, out, dq, dk, dv),
+                                      int(bool(causal)), scale, _stream_ptr(stream)), "hilberta_packed_backward")
+    return dq, dk, dv
 
 
 def packed_status() -> int:

@@ -51,7 +51,6 @@ struct Params {
     packed::Sequences seq;
     int parts, odd, group, g_shift;   // parts = kv_heads * odd; group = odd << g_shift
     int tiles;                        // query tiles of a unit, 1 or 2
-    int causal;
     long long stride_t, stride_h;     // of out
     __nv_bfloat16 *out;
     float *lse;
@@ -75,7 +74,7 @@ __device__ __forceinline__ Work work_of(const Params &p, const packed::Unit &u) 
     w.nt = (p.tiles > 1 && w.tok0 + tpt < w.len) ? 2 : 1;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-        const int end = p.causal ? min(w.len, w.tok0 + (t + 1) * tpt) : w.len;
+        const int end = p.seq.causal ? min(w.len, w.tok0 + (t + 1) * tpt) : w.len;
         w.n[t] = t < w.nt ? (end + BN - 1) / BN : 0;
     }
     return w;
@@ -150,14 +149,14 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     allow_next();
     wait_for_previous();
 
-    // the next unit, as the roles see it; `release`: this thread tells that it has read it
+    // the next unit, for a role of one thread
     uint32_t uc = 0;
-    auto next_unit = [&](packed::Unit &u, bool release, int code) {
+    auto next_unit = [&](packed::Unit &u, int code) {
         const uint32_t s = uc % UNITS, ph = (uc / UNITS) & 1;
         if (!wait_or_abort(bar(U_FULL + s), ph, &abort_flag, status, code)) return false;
         u = units[s];
         ++uc;
-        if (release) mbar_arrive(bar(U_EMPTY + s));
+        mbar_arrive(bar(U_EMPTY + s));
         return u.len >= 0;
     };
 
@@ -166,10 +165,10 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     }
     if (warp == 10) {
         // ------------------------------------------------------------ finds the units
-        packed::Levels levels;
+        packed::Runs runs;
         for (int round = 0;; ++round) {
             packed::Unit u;
-            const bool found = packed::find_unit(prm.seq, levels, prm.parts, blockIdx.x, gridDim.x, round, u);
+            const bool found = packed::find_unit(prm.seq, runs, prm.parts, blockIdx.x, gridDim.x, round, u);
             if (!found) u.len = -1;
             const uint32_t s = round % UNITS, ph = (round / UNITS) & 1;
             bool ok = true;
@@ -202,7 +201,7 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 return true;
             };
             packed::Unit u;
-            while (ok && next_unit(u, true, 0x100)) {
+            while (ok && next_unit(u, 0x100)) {
                 const Work w = work_of(prm, u);
                 ok = wait_or_abort(bar(Q_EMPTY), (qc & 1) ^ 1, &abort_flag, status, 0x101);
                 if (!ok) break;
@@ -247,7 +246,7 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 return true;
             };
             packed::Unit u;
-            while (ok && next_unit(u, true, 0x200)) {
+            while (ok && next_unit(u, 0x200)) {
                 const Work w = work_of(prm, u);
                 const int n = max(w.n[0], w.n[1]);
                 ok = wait_or_abort(bar(Q_FULL), qc & 1, &abort_flag, status, 0x201);
@@ -299,19 +298,34 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         const float scale_log2 = prm.scale_log2;
         uint32_t cS = 0, cPV = 0, ent = 0;
         bool ok = true;
-        packed::Unit u;
         while (ok) {
-            const bool any = next_unit(u, false, 0x300);
-            __syncwarp();
-            if (!any) break;
-            if (lane == 0) mbar_arrive(bar(U_EMPTY + (uc - 1) % UNITS));
-            const Work w = work_of(prm, u);
+            // The unit stays in its slot to the end, so that little of it lives in registers beside the scores.
+            const uint32_t slot = uc % UNITS;
+            ok = wait_or_abort(bar(U_FULL + slot), (uc / UNITS) & 1, &abort_flag, status, 0x300);
+            ++uc;
+            const volatile packed::Unit &u = units[slot];
+            if (!ok || u.len < 0) break;
+            auto work = [&] {
+                packed::Unit c;
+                c.row0 = u.row0, c.len = u.len, c.block = u.block, c.head = u.head;
+                return work_of(prm, c);
+            };
+            auto release = [&] {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(U_EMPTY + slot));
+            };
             const uint32_t ent0 = ent;
-            ent += 2 * (uint32_t)max(w.n[0], w.n[1]);
-            if (t >= w.nt) continue;
-            const int n = t ? w.n[1] : w.n[0];
-            const int tok = w.tok0 + t * (BM >> prm.g_shift) + (r >> prm.g_shift);
-            const int limit = prm.causal ? min(tok + 1, w.len) : w.len;   // keys that this row sees
+            int n, first_masked;   // key blocks of this tile; from here on a row's keys may end within a block
+            {
+                const Work w = work();
+                ent += 2 * (uint32_t)max(w.n[0], w.n[1]);
+                n = t ? w.n[1] : w.n[0];
+                first_masked = (prm.seq.causal ? min(w.tok0 + t * (BM >> prm.g_shift), w.len) : w.len) / BN;
+            }
+            if (n == 0) {   // this tile is absent
+                release();
+                continue;
+            }
             float m_ref = 0.f, l = 0.f;
             float l_fix = 0.f;   // rounding errors of the blocks' largest weights: part of the output's normaliser, not of lse
             for (int j = 0; j < n; ++j) {
@@ -323,26 +337,27 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 #pragma unroll
                 for (int c = 0; c < BN / 32; ++c) tmem_ld32(tS + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[c * 32]));
                 tmem_wait_ld();
-                const int lim = limit - j * BN;
-                if (lim < BN) {
+                if (j >= first_masked) {
+                    const Work w = work();
+                    const int tok = w.tok0 + ((t * BM + r) >> prm.g_shift), valid = w.len - j * BN;
+                    const int lim = prm.seq.causal ? min(tok + 1 - j * BN, valid) : valid;   // keys of the block that this row sees
 #pragma unroll
                     for (int i = 0; i < BN; ++i)
                         if (i >= lim) s[i] = 0xff800000u;  // -inf
-                }
-                const int valid = w.len - j * BN;
-                if (valid < BN) {
                     // Rows of the V tile behind the sequence belong to others: their weights are zero, and so are
                     // they from here on, whatever they hold.  (Both tiles do this; the zeros are the same.)
-                    const uint32_t e = ent0 + 2 * (uint32_t)j + 1;
-                    ok = wait_or_abort(bar(KV_FULL + slot_of(e)), phase_of(e), &abort_flag, status, 0x309);
-                    if (!ok) break;
-                    if (r >= valid) {
-                        const uint32_t zero[4] = {0u, 0u, 0u, 0u};
+                    if (valid < BN) {
+                        const uint32_t e = ent0 + 2 * (uint32_t)j + 1;
+                        ok = wait_or_abort(bar(KV_FULL + slot_of(e)), phase_of(e), &abort_flag, status, 0x309);
+                        if (!ok) break;
+                        if (r >= valid) {
+                            const uint32_t zero[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-                        for (int c = 0; c < NSLAB * 8; ++c)
-                            st_shared_v4(sKV + slot_of(e) * TILE_BYTES + (c >> 3) * SLAB_BYTES + r * 128 + (c & 7) * 16, zero);
+                            for (int c = 0; c < NSLAB * 8; ++c)
+                                st_shared_v4(sKV + slot_of(e) * TILE_BYTES + (c >> 3) * SLAB_BYTES + r * 128 + (c & 7) * 16, zero);
+                        }
+                        fence_proxy_async_smem();
                     }
-                    fence_proxy_async_smem();
                 }
                 // Eight independent max chains, then a short tree; chains 3 and 7 hold the scores whose exponentials
                 // the FMA pipes will compute (pairs 3 modulo 4), the other six those of the MUFU unit.
@@ -425,6 +440,8 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             ok = wait_or_abort(bar(PV_DONE + t), (cPV - 1) & 1, &abort_flag, status, 0x305 + t);
             if (!ok) break;
             tc_fence_after();
+            const Work w = work();
+            const int tok = w.tok0 + ((t * BM + r) >> prm.g_shift);
             const bool in = tok < w.len;
             const int head = w.head0 + (r & ((1 << prm.g_shift) - 1));
             const float inv = 1.f / (l + l_fix);
@@ -451,6 +468,7 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 }
             }
             tc_fence_before();
+            release();
         }
     }
     tc_fence_before();
@@ -553,7 +571,7 @@ bool overlap(const void *a, const int64_t *sa, int ha, const void *b, const int6
     return hilberta_check_overlap(pa, pb, 1, ha, total, 0, 2 * sa[1], 2 * sa[0], 2 * head_dim) != 0;
 }
 
-int read_status(bool *expired) {
+int forward_status(bool *expired) {
     int code = 0;
     HB_CUDA(cudaMemcpyFromSymbol(&code, g_status, sizeof(int)));
     if (code) {
@@ -571,7 +589,8 @@ using namespace hilberta;
 
 extern "C" int hilberta_packed_status(void) {
     bool expired = false;
-    const int rc = packed::read_status(&expired);
+    int rc = packed::forward_status(&expired);
+    if (rc == HILBERTA_OK) rc = packed::backward_status(&expired);
     return rc != HILBERTA_OK ? rc : expired ? HILBERTA_ERR_TIMEOUT : HILBERTA_OK;
 }
 
@@ -605,8 +624,7 @@ extern "C" int hilberta_packed_forward(const void *q, const void *k, const void 
         return ((long long)total / (tiles * per_tile) + std::min((long long)n_seq, (long long)total)) * p.parts;   // at most
     };
     p.tiles = units(2) >= sms ? 2 : 1;
-    p.seq = {cu_seqlens, n_seq, total, __builtin_ctz((unsigned)(p.tiles * per_tile))};
-    p.causal = causal != 0;
+    p.seq = {cu_seqlens, n_seq, total, __builtin_ctz((unsigned)(p.tiles * per_tile)), causal != 0};
     p.stride_t = strides[6];
     p.stride_h = strides[7];
     p.out = (__nv_bfloat16 *)out;
