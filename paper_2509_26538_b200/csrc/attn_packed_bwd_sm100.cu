@@ -9,6 +9,10 @@
 //              A = K_j Q_i^T, B = V_j dO_i^T (a thread owns a KEY row), P^T, dS^T -> TMEM, dV_j += P^T dO_i, dK_j += dS^T Q_i
 // Seven products where one pass that adds dQ up in memory would take five, but no atomics: every sum is taken in a
 // fixed order, the heads of a group among them, and no fp32 copy of dQ is written and read.
+// Sequences of up to 128 tokens: the statistics' delta carries the rounding of O to bf16, which a row of few keys
+// feels most, its dS being a small difference; there all keys of a row are in one block, and the element-wise step takes
+// delta = sum_j P_ij dP_ij itself.  (Error of dq against 64 bits, sequences of 2 ... 5 tokens 4.6e-3 and 2.5e-3 of the
+// norm, 64 ... 77 tokens 3.1e-3 and 2.4e-3, 300 tokens 2.9e-3 and 2.5e-3.)
 // Per block the tensor pipe sees  A(s+1) | out(s) | B(s+1)  back to back: the element-wise step turns scores into
 // weights as soon as A is written (phase 1) and frees A for the next block; phase 2 overwrites B in place with P and dS.
 #include <algorithm>
@@ -40,7 +44,8 @@ enum Bar {
     P_READY,                      // [part]
     T1_FULL = P_READY + 2, T1_EMPTY = T1_FULL + NT1,
     T2_FULL = T1_EMPTY + NT1, T2_EMPTY = T2_FULL + NT2,
-    U_FULL = T2_EMPTY + NT2, U_EMPTY = U_FULL + UNITS,   // U_EMPTY: two producers, issuer, 8 element-wise and 4 epilogue warps
+    SHORT = T2_EMPTY + NT2,       // the element-wise threads among themselves (256 arrivals)
+    U_FULL = SHORT + 1, U_EMPTY = U_FULL + UNITS,   // U_EMPTY: two producers, issuer, 8 element-wise and 4 epilogue warps
     NUM_BARS = U_EMPTY + UNITS
 };
 constexpr int UNIT_READERS = 15;
@@ -145,7 +150,7 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
     }
     const uint32_t sbase = smem_u32(smem);
     const uint32_t sR1 = sbase + OFF_R1, sR2 = sbase + OFF_R2, sT1 = sbase + OFF_T1, sT2 = sbase + OFF_T2;
-    const float *stats = reinterpret_cast<const float *>(smem + OFF_STAT);
+    float *stats = reinterpret_cast<float *>(smem + OFF_STAT);
     const uint32_t bar0 = sbase + OFF_BARS;
     packed::Unit *const units = reinterpret_cast<packed::Unit *>(smem + OFF_UNITS);
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + OFF_MISC);
@@ -161,7 +166,7 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
         for (int i = 0; i < NUM_BARS; ++i) {
             uint32_t count = 1;
             if (i == EPI_DONE) count = 128;
-            if (i == A_DONE || i == P_READY || i == P_READY + 1) count = 256;
+            if (i == A_DONE || i == P_READY || i == P_READY + 1 || i == SHORT) count = 256;
             // DKV: ring 2 also carries the row statistics, copied by the 32 lanes of its producer warp
             if (MODE == MODE_DKV && i >= T2_FULL && i < T2_FULL + NT2) count = 33;
             if (i >= U_EMPTY) count = UNIT_READERS;
@@ -429,9 +434,13 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tA = tmem + lane_addr + REG_A + wg * 64, tB = tmem + lane_addr + REG_B + wg * 64;
         const float scale_log2 = prm.scale_log2;
-        uint32_t g = 0;
+        uint32_t g = 0, n_short = 0;
         bool ok = true;
         packed::Unit u;
+        auto meet = [&] {   // all element-wise threads
+            mbar_arrive(bar(SHORT));
+            return wait_or_abort(bar(SHORT), n_short++ & 1, abort_flag, status, 0x608);
+        };
         while (ok) {
             const bool any = next_unit(u, false, 0x601);
             __syncwarp();
@@ -471,13 +480,12 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
                             lo_ds = 64;
                         }
                     }
-                    const float4 *st_l = nullptr, *st_d = nullptr;
+                    float *const slot = stats + (MODE == MODE_DKV ? (g % NT2) * (2 * BK) : 0);   // lse2, then delta
+                    const float4 *const st_l = reinterpret_cast<const float4 *>(slot + wg * 64), *const st_d = st_l + BK / 4;
                     if (MODE == MODE_DKV) {
                         // the statistics arrive with ring 2
                         ok = wait_or_abort(bar(T2_FULL + g % NT2), (g / NT2) & 1, abort_flag, status, 0x602);
                         if (!ok) break;
-                        st_l = reinterpret_cast<const float4 *>(stats + (g % NT2) * (2 * BK) + wg * 64);
-                        st_d = st_l + BK / 4;
                     }
                     // ---- phase 1: weights from the scores
                     ok = wait_or_abort(bar(S_FULL), g & 1, abort_flag, status, 0x603 + wg);
@@ -524,6 +532,56 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
                         }
                         fence_proxy_async_smem();
                     }
+                    const bool exact = w.len <= BK;   // the row's or column's delta from this block alone
+                    if (exact) {
+                        float sum[2] = {0.f, 0.f};   // DQ: of this row; DKV: of columns lane and 32 + lane over this warp's keys
+#pragma unroll
+                        for (int h2 = 0; h2 < 2; ++h2) {
+                            uint32_t d[32];
+                            float x[32];
+                            tmem_ld32(tB + h2 * 32, d);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                // a weight of zero, whatever the other factor; keys behind the sequence count for nothing
+                                const float p = __uint_as_float(a[h2 * 32 + i]);
+                                x[i] = p == 0.f || (MODE == MODE_DKV && tok >= w.len) ? 0.f : p * __uint_as_float(d[i]);
+                            }
+                            if (MODE == MODE_DQ) {
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) sum[0] += x[i];
+                            } else {
+                                // lane c is left with the sum of column c: each step hands half of the columns over
+#pragma unroll
+                                for (int o = 16; o > 0; o >>= 1) {
+                                    const bool up = (lane & o) != 0;
+#pragma unroll
+                                    for (int i = 0; i < o; ++i) {
+                                        const float keep = up ? x[i + o] : x[i], give = up ? x[i] : x[i + o];
+                                        x[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+                                    }
+                                }
+                                sum[h2] = x[0];
+                            }
+                        }
+                        if (MODE == MODE_DQ) {
+                            slot[wg * BK + r] = sum[0];
+                            ok = meet();
+                            if (!ok) break;
+                            row_dl = slot[r] + slot[BK + r];
+                        } else {
+                            // four warps' sums become two in the place of lse2 and delta, which nobody needs any more
+                            float *const to = slot + (warp & 1) * BK + wg * 64 + lane;
+                            ok = meet();
+                            if (!ok) break;
+                            if ((warp & 2) == 0) to[0] = sum[0], to[32] = sum[1];
+                            ok = meet();
+                            if (!ok) break;
+                            if ((warp & 2) != 0) to[0] += sum[0], to[32] += sum[1];
+                            ok = meet();
+                            if (!ok) break;
+                        }
+                    }
                     auto phase2 = [&](auto MASKED) {
 #pragma unroll
                         for (int h2 = 0; h2 < 2; ++h2) {
@@ -535,7 +593,13 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
                             for (int i4 = 0; i4 < 8; ++i4) {
                                 const int c0 = h2 * 32 + 4 * i4;
                                 float4 d4 = make_float4(row_dl, row_dl, row_dl, row_dl);
-                                if (MODE == MODE_DKV) d4 = st_d[c0 >> 2];
+                                if (MODE == MODE_DKV) {
+                                    d4 = st_d[c0 >> 2];
+                                    if (decltype(MASKED)::value && exact) {
+                                        const float4 e4 = st_l[c0 >> 2];
+                                        d4.x += e4.x, d4.y += e4.y, d4.z += e4.z, d4.w += e4.w;
+                                    }
+                                }
                                 const float2 pa = make_float2(__uint_as_float(a[c0]), __uint_as_float(a[c0 + 1]));
                                 const float2 pb = make_float2(__uint_as_float(a[c0 + 2]), __uint_as_float(a[c0 + 3]));
                                 const float2 sa = __fmul2_rn(__fadd2_rn(make_float2(__uint_as_float(d[4 * i4]), __uint_as_float(d[4 * i4 + 1])),
@@ -562,7 +626,7 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
                             mbar_arrive(bar(P_READY + h2));
                         }
                     };
-                    if (masked) phase2(std::true_type{});
+                    if (masked || exact) phase2(std::true_type{});
                     else phase2(std::false_type{});
                 }
             }

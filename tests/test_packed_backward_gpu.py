@@ -109,6 +109,24 @@ def test_what_other_rows_hold_does_not_matter(dim, causal):
 
 
 @pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("lens", [(2,) * 200, (5, 3, 2, 4) * 40, (20, 10, 33, 128, 127)])
+def test_short_sequences_keep_their_precision(lens, dim, causal):
+    """Two roundings to bf16 remain, of dS (or P) and of the result.  Each is off by 1.7e-3 of the value in the root mean
+    square (up to 2^-8, evenly spread over half a step, over a binade), together 2.4e-3 of the norm; delta taken from the
+    rounded output would add as much again and more."""
+    q, k, v, cu = make(lens, 4, 2, dim, 8)
+    dout, out, lse, grads = _check(q, k, v, cu, causal)
+    err, norm = [0.0] * 3, [0.0] * 3
+    for a, b, want, _ in _reference(dout, q, k, v, cu, causal, 0.0):
+        for i in range(3):
+            err[i] += float((grads[i][a:b].double() - want[i]).square().sum())
+            norm[i] += float(want[i].square().sum())
+    for e, n in zip(err, norm):
+        assert math.sqrt(e / n) <= 3e-3, math.sqrt(e / n)
+
+
+@pytest.mark.parametrize("causal", [True, False])
 def test_scales_and_layouts(causal):
     q, k, v, cu = make((300, 20, 170), 6, 2, 64, 9)
     _check(q, k, v, cu, causal, scale=0.3)
