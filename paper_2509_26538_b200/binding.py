@@ -393,13 +393,9 @@ def hilberta_unpermute(src, dst, plan: Plan, stream=None):
 
 
 # ---- operators of the block around the attention ---------------------------------------------------------------
+# These calls take a few microseconds on the device, so their checks are written to cost little on the host.
 
-def _here(*tensors):
-    """The tensors live on the current CUDA device (the library launches there)."""
-    device = _current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise ValueError(f"tensor on {t.device}, the current device is cuda:{device}")
+_I64x6, _I64x8, _I64x16 = ctypes.c_int64 * 6, ctypes.c_int64 * 8, ctypes.c_int64 * 16
 
 
 def _current_device() -> int:
@@ -408,6 +404,14 @@ def _current_device() -> int:
     device = int(torch.cuda.current_device())   # initialises torch's side of CUDA if need be
     _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     return device
+
+
+def _here(*tensors):
+    """The tensors live on the current CUDA device (the library launches there)."""
+    device = _current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"tensor on {t.device}, the current device is cuda:{device}")
 
 
 def _scratch(n, like, stream):
@@ -423,14 +427,15 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _rows(t, name):
-    """(rows, row stride) of a [..., cols] tensor whose leading axes are one."""
-    if t.dim() < 1 or (t.shape[-1] > 1 and t.stride(-1) != 1):
-        raise ValueError(f"{name}: the last axis has to be contiguous")
+def _row_stride(t, name):
+    """The row stride of a [..., cols] tensor whose leading axes are one."""
+    shape = t.shape
     if t.is_contiguous():
-        return t.numel() // max(t.shape[-1], 1), t.shape[-1]
+        return shape[-1]
+    if t.dim() < 1 or (shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name}: the last axis has to be contiguous")
     rows, stride = 1, 0
-    for n, st in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+    for n, st in zip(reversed(shape[:-1]), reversed(t.stride()[:-1])):
         if n == 1:
             continue
         if rows > 1 and st != rows * stride:
@@ -438,31 +443,32 @@ def _rows(t, name):
         if rows == 1:
             stride = st
         rows *= n
-    return rows, max(stride, t.shape[-1])
+    return max(stride, shape[-1])
 
 
-def _norm_weights(x, tensors):
-    """(rows per group, row stride, dtype code) of the weight-like tensors [cols] or [groups, cols]."""
-    given = [t for t in tensors if t is not None]
-    if not given:
+def _norm_weights(x, a, b):
+    """(rows per group, row stride, dtype code) of weight and bias, or of their gradients: [cols] or [groups, cols]."""
+    w = a if a is not None else b
+    if w is None:
         return 0, 0, _dtype_code(x)
-    w = given[0]
-    cols = x.shape[-1]
-    for t in given:
-        if t.shape != w.shape or t.dtype != w.dtype or t.shape[-1] != cols or (cols > 1 and t.stride(-1) != 1):
-            raise ValueError("weight, bias and their gradients: one shape and dtype, [cols] or [groups, cols]")
-    if w.dim() == 1:
+    shape, cols = w.shape, x.shape[-1]
+    if b is not None and b is not w and (b.shape != shape or b.dtype != w.dtype or b.stride() != w.stride()):
+        raise ValueError("weight and bias (and their gradients): one shape, dtype and row stride")
+    if shape[-1] != cols or (cols > 1 and w.stride(-1) != 1):
+        raise ValueError("weights are [cols] or [groups, cols], the last axis contiguous")
+    if len(shape) == 1:
         return 0, cols, _dtype_code(w)
-    if w.dim() != 2 or x.dim() < 2 or w.shape[0] != x.shape[0]:
+    if len(shape) != 2 or x.dim() < 2 or shape[0] != x.shape[0]:
         raise ValueError("weights of a group of rows are [x.shape[0], cols]")
-    groups = w.shape[0]
+    groups = shape[0]
     per = x.numel() // (cols * groups) if groups and cols else 0
     return (0 if groups == 1 else per), w.stride(0), _dtype_code(w)
 
 
-def _same_stride(a, b, what):
-    if a is not None and b is not None and a.dim() == 2 and a.shape[0] > 1 and a.stride(0) != b.stride(0):
-        raise ValueError(f"{what} have to share a row stride")
+def _statistics(x, rows, mean, rstd):
+    for t in (mean, rstd):
+        if t is not None and (t.numel() != rows or not t.is_contiguous() or _dtype_code(t) != FP32):
+            raise ValueError("mean and rstd: contiguous fp32, one element for each row of x")
 
 
 def layer_norm(x, weight, bias, y, mean=None, rstd=None, eps=1e-6, unit_offset=False, stream=None):
@@ -470,62 +476,55 @@ def layer_norm(x, weight, bias, y, mean=None, rstd=None, eps=1e-6, unit_offset=F
 
     weight, bias: None, [cols], or [x.shape[0], cols] (one row per sample).  mean, rstd: None or fp32 [...] to be
     written for layer_norm_backward.  y may be x."""
-    rows, sx = _rows(x, "x")
-    _, sy = _rows(y, "y")
     if y.shape != x.shape or y.dtype != x.dtype:
         raise ValueError("x and y must match")
-    _statistics(x, mean, rstd)
-    per, sw, wcode = _norm_weights(x, (weight, bias))
-    _same_stride(weight, bias, "weight and bias")
+    sx, sy, cols = _row_stride(x, "x"), _row_stride(y, "y"), x.shape[-1]
+    rows = x.numel() // cols if cols else 0
+    _statistics(x, rows, mean, rstd)
+    per, sw, wcode = _norm_weights(x, weight, bias)
     _here(x, y, weight, bias, mean, rstd)
-    _check(lib().hilberta_layer_norm(x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), _ptr(mean), _ptr(rstd), rows,
-                                     x.shape[-1], per, sx, sy, sw, _dtype_code(x), wcode, int(bool(unit_offset)), eps,
-                                     _stream_ptr(stream)), "hilberta_layer_norm")
+    status = lib().hilberta_layer_norm(x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), _ptr(mean), _ptr(rstd), rows, cols, per, sx,
+                                       sy, sw, _dtype_code(x), wcode, 1 if unit_offset else 0, eps, _stream_ptr(stream))
+    if status:
+        _check(status, "hilberta_layer_norm")
     return y, mean, rstd
-
-
-def _statistics(x, *tensors):
-    for t in tensors:
-        if t is not None and (t.shape != x.shape[:-1] or not t.is_contiguous() or _dtype_code(t) != FP32):
-            raise ValueError("mean and rstd: contiguous fp32 of x's shape without the last axis")
 
 
 def layer_norm_workspace(x, weight=None) -> int:
     """Bytes of workspace that layer_norm_backward needs for x and weight (or one of their gradients)."""
-    per = _norm_weights(x, (weight,))[0]
-    return int(lib().hilberta_layer_norm_workspace(x.numel() // max(x.shape[-1], 1), x.shape[-1], per))
+    cols = x.shape[-1]
+    return int(lib().hilberta_layer_norm_workspace(x.numel() // max(cols, 1), cols, _norm_weights(x, weight, None)[0]))
 
 
 def layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, unit_offset=False, workspace=None, stream=None):
     """Gradients of layer_norm into dx, dweight, dbias (any may be None, not all).  workspace: None (taken from torch's
     allocator) or a uint8 tensor of layer_norm_workspace() bytes."""
-    rows, sx = _rows(x, "x")
-    _, sdy = _rows(dy, "dy")
-    sdx = 0
-    if dx is not None:
-        sdx = _rows(dx, "dx")[1]
-    for t in (dy, dx):
-        if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
-            raise ValueError("dy, x and dx must match")
+    if dy.shape != x.shape or dy.dtype != x.dtype or (dx is not None and (dx.shape != x.shape or dx.dtype != x.dtype)):
+        raise ValueError("dy, x and dx must match")
     if mean is None or rstd is None:
         raise ValueError("mean and rstd of the forward pass are needed")
-    _statistics(x, mean, rstd)
-    per, _, wcode = _norm_weights(x, (weight, dweight, dbias))
-    sw = weight.stride(0) if weight is not None and weight.dim() == 2 else 0
-    g = dweight if dweight is not None else dbias
-    sdw = g.stride(0) if g is not None and g.dim() == 2 else 0
-    _same_stride(dweight, dbias, "dweight and dbias")
+    sdy, sx, cols = _row_stride(dy, "dy"), _row_stride(x, "x"), x.shape[-1]
+    sdx = 0 if dx is None else _row_stride(dx, "dx")
+    rows = x.numel() // cols if cols else 0
+    _statistics(x, rows, mean, rstd)
+    per, sw, wcode = _norm_weights(x, weight, None)
+    sdw = 0
+    if dweight is not None or dbias is not None:
+        gper, sdw, gcode = _norm_weights(x, dweight, dbias)
+        if weight is not None and (gper != per or gcode != wcode):
+            raise ValueError("a weight and its gradient: one shape and dtype")
+        per, wcode = gper, gcode
+        if workspace is None:
+            n = lib().hilberta_layer_norm_workspace(rows, cols, per)
+            if n:
+                workspace = _scratch(n, x, stream)
     _here(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace)
-    L = lib()
-    if workspace is None and g is not None:
-        n = int(L.hilberta_layer_norm_workspace(rows, x.shape[-1], per))
-        if n:
-            workspace = _scratch(n, x, stream)
-    _check(L.hilberta_layer_norm_backward(dy.data_ptr(), x.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(), _ptr(dx),
-                                          _ptr(dweight), _ptr(dbias), _ptr(workspace),
-                                          0 if workspace is None else workspace.numel() * workspace.element_size(), rows,
-                                          x.shape[-1], per, sdy, sx, sdx, sw, sdw, _dtype_code(x), wcode,
-                                          int(bool(unit_offset)), _stream_ptr(stream)), "hilberta_layer_norm_backward")
+    status = lib().hilberta_layer_norm_backward(dy.data_ptr(), x.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(), _ptr(dx),
+                                                _ptr(dweight), _ptr(dbias), _ptr(workspace), 0 if workspace is None else workspace.nbytes,
+                                                rows, cols, per, sdy, sx, sdx, sw, sdw, _dtype_code(x), wcode, 1 if unit_offset else 0,
+                                                _stream_ptr(stream))
+    if status:
+        _check(status, "hilberta_layer_norm_backward")
     return dx, dweight, dbias
 
 
@@ -538,35 +537,43 @@ def rotary_frequencies(pairs, base=10000.0, scaling=ROTARY_PLAIN, scale=1.0, con
     return f, factor.value
 
 
+_host_types = []   # torch's fp64 and int32, filled by the first call
+
+
 def _rotary(fn, name, x, out, inv_freq, positions, axis, interleaved, factor, plan, stream):
-    import torch
-    if x.dim() != 4 or out.shape != x.shape or out.dtype != x.dtype:
+    if not _host_types:
+        import torch
+        _host_types.extend((torch.float64, torch.int32))
+    f64, int32 = _host_types
+    shape, sx, so = x.shape, x.stride(), out.stride()
+    if len(shape) != 4 or out.shape != shape or out.dtype != x.dtype:
         raise ValueError("x and out: [batch, heads, S, head_dim], one shape and dtype")
-    B, H, S, D = x.shape
-    if D > 1 and (x.stride(3) != 1 or out.stride(3) != 1):
+    B, H, S, D = shape
+    if D > 1 and (sx[3] != 1 or so[3] != 1):
         raise ValueError("the head_dim axis has to be contiguous")
-    if inv_freq.dtype != torch.float64 or inv_freq.is_cuda or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+    if inv_freq.dtype != f64 or inv_freq.is_cuda or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
         raise ValueError("inv_freq: contiguous fp64 [pairs] on the CPU")
     axes, pos_stride = 1, 0
-    if axis is not None and (axis.dtype != torch.int32 or axis.is_cuda or axis.shape != inv_freq.shape or not axis.is_contiguous()):
+    if axis is not None and (axis.dtype != int32 or axis.is_cuda or axis.shape != inv_freq.shape or not axis.is_contiguous()):
         raise ValueError("axis: contiguous int32 [pairs] on the CPU")
     if positions is not None:
-        if positions.dtype != torch.int32 or not positions.is_contiguous():
+        if positions.dtype != int32 or not positions.is_contiguous():
             raise ValueError("positions: contiguous int32")
-        shape = tuple(positions.shape)
+        ps = tuple(positions.shape)
         if axis is not None:
-            if not shape:
+            if not ps:
                 raise ValueError("positions: [S, axes] or [batch, S, axes]")
-            axes, shape = shape[-1], shape[:-1]
-        if shape == (B, S):
+            axes, ps = ps[-1], ps[:-1]
+        if ps == (B, S):
             pos_stride = S
-        elif shape != (S,):
+        elif ps != (S,):
             raise ValueError("positions: [S] or [batch, S], with an axis for each position axis if `axis` is given")
     _here(x, out, positions)
-    strides = (ctypes.c_int64 * 6)(x.stride(0), x.stride(1), x.stride(2), out.stride(0), out.stride(1), out.stride(2))
-    _check(fn(x.data_ptr(), out.data_ptr(), _ptr(positions), inv_freq.data_ptr(), _ptr(axis), inv_freq.numel(), axes,
-              int(bool(interleaved)), factor, None if plan is None else plan._h, B, H, S, D, _dtype_code(x), strides, pos_stride,
-              _stream_ptr(stream)), name)
+    status = fn(x.data_ptr(), out.data_ptr(), _ptr(positions), inv_freq.data_ptr(), _ptr(axis), inv_freq.numel(), axes,
+                1 if interleaved else 0, factor, None if plan is None else plan._h, B, H, S, D, _dtype_code(x),
+                _I64x6(sx[0], sx[1], sx[2], so[0], so[1], so[2]), pos_stride, _stream_ptr(stream))
+    if status:
+        _check(status, name)
     return out
 
 
@@ -583,48 +590,49 @@ def rotary_backward(dout, dx, inv_freq, positions=None, axis=None, interleaved=F
                    factor, plan, stream)
 
 
-def _packed_shapes(q, k, v, like_q, like_k, lse, cu_seqlens):
-    """(total, heads, kv_heads, head_dim) of packed tensors [total, heads, head_dim]; checks the others against them."""
-    import torch
-    if q.dim() != 3 or k.dim() != 3:
-        raise ValueError("packed tensors are [total, heads, head_dim]")
-    T, H, D = q.shape
-    Hk = k.shape[1]
-    for ts, shape in (((q,) + like_q, (T, H, D)), ((k, v) + like_k, (T, Hk, D))):
+def _packed_args(like_q, like_k, lse, cu_seqlens):
+    """(total, heads, kv_heads, head_dim) of packed tensors, those of q's shape and those of k's, and their strides."""
+    if not _host_types:
+        import torch
+        _host_types.extend((torch.float64, torch.int32))
+    q, k = like_q[0], like_k[0]
+    qs, ks, dtype, strides = q.shape, k.shape, q.dtype, []
+    if len(qs) != 3 or len(ks) != 3 or qs[0] != ks[0] or qs[2] != ks[2]:
+        raise ValueError("packed tensors are [total, heads, head_dim] and [total, kv_heads, head_dim]")
+    T, H, D = qs
+    device = _current_device()
+    for ts, shape in ((like_q, qs), (like_k, ks)):
         for t in ts:
-            if t.shape != shape or t.dtype != q.dtype:
-                raise ValueError("packed tensors must match: [total, heads, head_dim] and [total, kv_heads, head_dim], one dtype")
-            if D > 1 and t.stride(2) != 1:
+            if t.shape != shape or t.dtype != dtype:
+                raise ValueError("packed tensors must match: one shape for q's kind and one for k's, one dtype")
+            st, sh, sd = t.stride()
+            if sd != 1 and D > 1:
                 raise ValueError("the head_dim axis has to be contiguous")
-    if lse is not None and (lse.shape != (H, T) or not lse.is_contiguous() or lse.dtype != torch.float32):
+            if t.get_device() != device:
+                raise ValueError(f"tensor on {t.device}, the current device is cuda:{device}")
+            if shape[1] == 1:   # an axis of one element has any stride
+                sh = (D + 7) // 8 * 8
+            if T <= 1:
+                st = max(shape[1] * sh, 8)
+            strides += (st, sh)
+    if lse is not None and (lse.shape != (H, T) or not lse.is_contiguous() or _dtype_code(lse) != FP32):
         raise ValueError("lse: contiguous fp32 [heads, total]")
-    if cu_seqlens.dtype != torch.int32 or cu_seqlens.dim() != 1 or not cu_seqlens.is_contiguous() or cu_seqlens.numel() < 1:
+    if cu_seqlens.dtype != _host_types[1] or cu_seqlens.dim() != 1 or not cu_seqlens.is_contiguous() or cu_seqlens.numel() < 1:
         raise ValueError("cu_seqlens: contiguous int32 [sequences + 1]")
-    _here(q, k, v, lse, cu_seqlens, *like_q, *like_k)
-    return T, H, Hk, D
-
-
-def _packed_strides(*tensors):
-    """(token, head) strides of each; an axis of one element has any."""
-    out = []
-    for t in tensors:
-        st, sh = t.stride(0), t.stride(1)
-        D = t.shape[2]
-        if t.shape[1] == 1:
-            sh = (D + 7) // 8 * 8
-        if t.shape[0] <= 1:
-            st = max(t.shape[1], 1) * max(sh, 1)
-        out += [st, sh]
-    return (ctypes.c_int64 * len(out))(*out)
+    _here(lse, cu_seqlens)
+    return T, H, ks[1], D, strides
 
 
 def packed_forward(q, k, v, out, cu_seqlens, lse=None, causal=True, scale=0.0, stream=None):
     """Attention within each of the sequences packed along the first axis: q, out [total, heads, head_dim], k, v
     [total, kv_heads, head_dim] bf16; cu_seqlens int32 [sequences + 1] on the device; lse None or fp32 [heads, total]."""
-    T, H, Hk, D = _packed_shapes(q, k, v, (out,), (), lse, cu_seqlens)
-    _check(lib().hilberta_packed_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse), cu_seqlens.data_ptr(),
-                                         cu_seqlens.numel() - 1, T, H, Hk, D, _dtype_code(q), _packed_strides(q, k, v, out),
-                                         int(bool(causal)), scale, _stream_ptr(stream)), "hilberta_packed_forward")
+    T, H, Hk, D, st = _packed_args((q, out), (k, v), lse, cu_seqlens)
+    status = lib().hilberta_packed_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse), cu_seqlens.data_ptr(),
+                                           cu_seqlens.numel() - 1, T, H, Hk, D, _dtype_code(q),
+                                           _I64x8(st[0], st[1], st[4], st[5], st[6], st[7], st[2], st[3]), 1 if causal else 0, scale,
+                                           _stream_ptr(stream))
+    if status:
+        _check(status, "hilberta_packed_forward")
     return out, lse
 
 
@@ -638,20 +646,23 @@ def packed_backward(dout, q, k, v, out, lse, dq, dk, dv, cu_seqlens, causal=True
     (taken from torch's allocator) or a uint8 tensor of packed_workspace() bytes."""
     if lse is None:
         raise ValueError("lse of the forward pass is needed")
-    T, H, Hk, D = _packed_shapes(q, k, v, (dout, out, dq), (dk, dv), lse, cu_seqlens)
-    L = lib()
+    T, H, Hk, D, st = _packed_args((dout, q, out, dq), (k, v, dk, dv), lse, cu_seqlens)
     if workspace is None:
-        workspace = _scratch(int(L.hilberta_packed_workspace(T, H)), q, stream)
-    _here(workspace)
-    _check(L.hilberta_packed_backward(dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
-                                      dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), workspace.data_ptr(),
-                                      workspace.numel() * workspace.element_size(), cu_seqlens.data_ptr(), cu_seqlens.numel() - 1,
-                                      T, H, Hk, D, _dtype_code(q), _packed_strides(dout, q, k, v, out, dq, dk, dv),
-                                      int(bool(causal)), scale, _stream_ptr(stream)), "hilberta_packed_backward")
+        workspace = _scratch(lib().hilberta_packed_workspace(T, H), q, stream)
+    else:
+        _here(workspace)
+    status = lib().hilberta_packed_backward(dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
+                                            dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+                                            cu_seqlens.data_ptr(), cu_seqlens.numel() - 1, T, H, Hk, D, _dtype_code(q),
+                                            _I64x16(st[0], st[1], st[2], st[3], st[8], st[9], st[10], st[11], st[4], st[5], st[6], st[7],
+                                                    st[12], st[13], st[14], st[15]), 1 if causal else 0, scale, _stream_ptr(stream))
+    if status:
+        _check(status, "hilberta_packed_backward")
     return dq, dk, dv
 
 
 def packed_status() -> int:
+    """0, or ERR_TIMEOUT if a wait inside a packed attention kernel has given up since the last call; synchronises."""
     return int(lib().hilberta_packed_status())
 
 

@@ -12,6 +12,7 @@
 #include <algorithm>
 
 #include "common.cuh"
+#include "sm100_ptx.cuh"
 
 namespace hilberta {
 namespace {
@@ -182,126 +183,295 @@ struct BackwardParams {
     long long rows, rows_per_group, stride_dy, stride_x, stride_dx, stride_w, stride_dw;
     int cols;
     float offset;
+    int stages, pitch;   // of the ring in shared memory
 };
 
-// A CTA's threads cover the columns (NV vectors of VEC each), so that the sums over rows stay in registers:
-// 2 NV VEC of them.  It takes R rows at a time: R is what keeps enough loads in flight, and one barrier serves the
-// 2 R sums over columns.  CTA (i, group) has rows i R ... of the group, then those gridDim.x R further on.
-template <class T, class W, int VEC, int NV, int R>
-__global__ void __launch_bounds__(VEC > 1 ? 512 : 1024)
-layer_norm_bwd_kernel(const BackwardParams prm) {
-    __shared__ float part[2][32][2 * R];
-    const int cols = prm.cols, warps = blockDim.x / 32, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+// weights as the gradients use them: w [+ 1], 1 without any
+template <class W, int VEC>
+__device__ __forceinline__ void load_weights(float *w, const W *p, bool given, float offset) {
+    Vec<W, VEC> v;
+    v.zero();
+    if (given) v.load(p);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) w[e] = given ? v.get(e) + offset : 1.f;
+}
+
+// this CTA's sum over its rows of dy n (which = 0) or dy (1) for one column: a partial sum, or the result
+template <class W>
+__device__ __forceinline__ void write_sum(const BackwardParams &prm, int which, int c, float sum) {
+    if (prm.partial) {
+        prm.partial[(((long long)blockIdx.y * gridDim.x + blockIdx.x) * 2 + which) * prm.cols + c] = sum;
+    } else if (void *to = which ? prm.dbias : prm.dweight) {
+        Vec<W, 1> o;
+        o.set(&sum);
+        o.store((W *)to + blockIdx.y * prm.stride_dw + c);
+    }
+}
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
+// Sums over columns need every element of a row, sums over rows one column of all: a thread keeps its columns for all
+// rows that its CTA sees (2 NV VEC fp32 sums in registers), and the two sums of a row cross the team that shares the row.
+
+// Rows of few vectors: a team of LANES <= 32 lanes has a row (one vector each, R rows at a time for loads in flight),
+// shuffles do the row sums and no barrier is needed until the teams' sums over rows are added up.
+template <class T, class W, int VEC, int LANES, int R>
+__global__ void __launch_bounds__(256)
+layer_norm_bwd_lanes_kernel(const BackwardParams prm) {
+    constexpr int TEAMS = 256 / LANES;
+    __shared__ float part[2][TEAMS][LANES * VEC + 1];
+    const int cols = prm.cols, lane = threadIdx.x % LANES, team = threadIdx.x / LANES, c = lane * VEC;
     const long long row_begin = (long long)blockIdx.y * prm.rows_per_group;
     const long long row_end = min(row_begin + prm.rows_per_group, prm.rows);
     const float inv_cols = 1.f / (float)cols;
-    float dw[NV * VEC] = {}, db[NV * VEC] = {};
-    Vec<W, VEC> w[NV];
+    const bool in = c < cols;
+    float dw[VEC] = {}, db[VEC] = {}, w[VEC];
     allow_next();
     wait_for_previous();
+    load_weights<W, VEC>(w, (const W *)prm.weight + blockIdx.y * prm.stride_w + c, prm.weight && in, prm.offset);
+    // a warp's teams stay together: the bound is that of the warp's first team
+    const long long step = (long long)gridDim.x * TEAMS * R;
+    for (long long r0 = row_begin + ((long long)blockIdx.x * TEAMS + team) * R; __any_sync(0xffffffffu, r0 < row_end); r0 += step) {
+        Vec<T, VEC> x[R], dy[R];
+        float mean[R], rstd[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const bool live = r0 + r < row_end;
+            x[r].zero();
+            dy[r].zero();
+            mean[r] = live ? prm.mean[r0 + r] : 0.f;
+            rstd[r] = live ? prm.rstd[r0 + r] : 0.f;
+            if (live && in) {
+                x[r].load((const T *)prm.x + (r0 + r) * prm.stride_x + c);
+                dy[r].load((const T *)prm.dy + (r0 + r) * prm.stride_dy + c);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float n[VEC], g[VEC], a = 0.f, b = 0.f;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float d = dy[r].get(e);
+                n[e] = (x[r].get(e) - mean[r]) * rstd[r];
+                g[e] = d * w[e];
+                if (in) {
+                    a += g[e];
+                    b = fmaf(g[e], n[e], b);
+                    dw[e] = fmaf(d, n[e], dw[e]);
+                    db[e] += d;
+                }
+            }
+            a = lanes_sum<LANES>(a) * inv_cols;
+            b = lanes_sum<LANES>(b) * inv_cols;
+            if (prm.dx && in && r0 + r < row_end) {
+                Vec<T, VEC> o;
+                float f[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) f[e] = rstd[r] * (g[e] - a - n[e] * b);
+                o.set(f);
+                o.store((T *)prm.dx + (r0 + r) * prm.stride_dx + c);
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+        part[0][team][c + e] = dw[e];
+        part[1][team][c + e] = db[e];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * cols; i += 256) {
+        const int which = i / cols, col = i % cols;
+        float sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < TEAMS; ++t) sum += part[which][t][col];
+        write_sum<W>(prm, which, col, sum);
+    }
+}
+
+// Longer rows: the CTA is the team.  R rows at a time come through a ring of shared memory, filled STAGES - 1 rounds
+// ahead by bulk copies (a register's worth of loads ahead left HBM idle at the barrier that the two row sums need), and
+// are read from there twice, for the sums and for dx.  A row that does not start on a 16-byte boundary is copied from the
+// boundary before to the one behind: the granules are those of its own first and last elements.
+constexpr int MAX_STAGES = 4;
+template <class T, class W, int VEC, int NV, int R>
+__global__ void __launch_bounds__(512)
+layer_norm_bwd_kernel(const BackwardParams prm) {
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ __align__(16) float part[2][16][2 * R];
+    __shared__ uint64_t full[MAX_STAGES];
+    const int cols = prm.cols, warps = blockDim.x / 32, warp = threadIdx.x / 32, lane = threadIdx.x % 32, stages = prm.stages;
+    const long long row_begin = (long long)blockIdx.y * prm.rows_per_group;
+    const long long row_end = min(row_begin + prm.rows_per_group, prm.rows);
+    const long long first = row_begin + (long long)blockIdx.x * R, step = (long long)gridDim.x * R;
+    const int rounds = first < row_end ? (int)((row_end - first + step - 1) / step) : 0;
+    const float inv_cols = 1.f / (float)cols;
+    const int pitch = prm.pitch;   // bytes of a row in the ring
+    float dw[NV * VEC] = {}, db[NV * VEC] = {};
+    float w[NV * VEC];
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < stages; ++i) ptx::mbar_init(ptx::smem_u32(&full[i]), 1);
+        ptx::mbar_fence_init();
+    }
+    allow_next();
+    wait_for_previous();
+    __syncthreads();
+    // x and dy of round i into its stage
+    auto fill = [&](int i) {
+        const int s = i % stages;
+        const uint32_t bar = ptx::smem_u32(&full[s]), to = ptx::smem_u32(ring) + (uint32_t)(s * 2 * R * pitch);
+        const long long r0 = first + i * step;
+        const int live = (int)min((long long)R, row_end - r0);
+        const T *src[2] = {(const T *)prm.x + r0 * prm.stride_x, (const T *)prm.dy + r0 * prm.stride_dy};
+        const long long stride[2] = {prm.stride_x, prm.stride_dy};
+        uint32_t bytes = 0;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            for (int r = 0; r < live; ++r) {
+                const uintptr_t at = (uintptr_t)(src[k] + r * stride[k]), from = at & ~(uintptr_t)15;
+                bytes += (uint32_t)((at + (size_t)cols * sizeof(T) + 15 & ~(uintptr_t)15) - from);
+            }
+        ptx::mbar_expect_tx(bar, bytes);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            for (int r = 0; r < live; ++r) {
+                const uintptr_t at = (uintptr_t)(src[k] + r * stride[k]), from = at & ~(uintptr_t)15;
+                bulk_load(to + (uint32_t)((k * R + r) * pitch), (const void *)from,
+                          (uint32_t)((at + (size_t)cols * sizeof(T) + 15 & ~(uintptr_t)15) - from), bar);
+            }
+    };
+    if (threadIdx.x == 0)
+        for (int i = 0; i < stages && i < rounds; ++i) fill(i);
     bool in[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = (i * (int)blockDim.x + (int)threadIdx.x) * VEC;
         in[i] = c < cols;
-        if (in[i] && prm.weight) w[i].load((const W *)prm.weight + blockIdx.y * prm.stride_w + c);
+        load_weights<W, VEC>(w + i * VEC, (const W *)prm.weight + blockIdx.y * prm.stride_w + c, prm.weight && in[i], prm.offset);
     }
-    auto weight = [&](int i, int e) { return prm.weight ? w[i].get(e) + prm.offset : 1.f; };
-    int k = 0;
-    for (long long r0 = row_begin + (long long)blockIdx.x * R; r0 < row_end; r0 += (long long)gridDim.x * R, k ^= 1) {
-        Vec<T, VEC> x[R][NV], dy[R][NV];
-        float mean[R], rstd[R], s[2 * R];
+    float mean_ahead[R], rstd_ahead[R];   // of the next round
+    auto statistics = [&](long long r0) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const bool live = r0 + r < row_end;
-            mean[r] = live ? prm.mean[r0 + r] : 0.f;
-            rstd[r] = live ? prm.rstd[r0 + r] : 0.f;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = (i * (int)blockDim.x + (int)threadIdx.x) * VEC;
-                if (live && in[i]) {
-                    x[r][i].load((const T *)prm.x + (r0 + r) * prm.stride_x + c);
-                    dy[r][i].load((const T *)prm.dy + (r0 + r) * prm.stride_dy + c);
-                } else {
-                    x[r][i].zero();
-                    dy[r][i].zero();
-                }
-            }
+            mean_ahead[r] = r0 + r < row_end ? prm.mean[r0 + r] : 0.f;
+            rstd_ahead[r] = r0 + r < row_end ? prm.rstd[r0 + r] : 0.f;
         }
+    };
+    statistics(first);
+    for (int i = 0; i < rounds; ++i) {
+        const int s = i % stages, k = i & 1;
+        const long long r0 = first + i * step;
+        const int live = (int)min((long long)R, row_end - r0);
+        float mean[R], rstd[R], sum[2 * R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            mean[r] = mean_ahead[r];
+            rstd[r] = rstd_ahead[r];
+        }
+        statistics(r0 + step);
+        const T *xs[R], *ds[R];   // the rows in the ring
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const uint8_t *base = ring + (size_t)s * 2 * R * pitch;
+            // VEC = 1: the offset within the granule
+            xs[r] = (const T *)(base + r * pitch + (VEC == 1 ? ((uintptr_t)((const T *)prm.x + (r0 + r) * prm.stride_x) & 15) : 0));
+            ds[r] = (const T *)(base + (R + r) * pitch + (VEC == 1 ? ((uintptr_t)((const T *)prm.dy + (r0 + r) * prm.stride_dy) & 15) : 0));
+        }
+        if (!ptx::mbar_wait(ptx::smem_u32(&full[s]), (i / stages) & 1)) return;   // never: the copy's bytes have been asked for
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             float a = 0.f, b = 0.f;
+            if (r < live) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                if (!in[i]) continue;
+                for (int v = 0; v < NV; ++v) {
+                    if (!in[v]) continue;
+                    const int c = (v * (int)blockDim.x + (int)threadIdx.x) * VEC;
+                    Vec<T, VEC> x, dy;
+                    x.load(xs[r] + c);
+                    dy.load(ds[r] + c);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float d = dy[r][i].get(e), n = (x[r][i].get(e) - mean[r]) * rstd[r];
-                    const float g = d * weight(i, e);
-                    a += g;
-                    b = fmaf(g, n, b);
-                    dw[i * VEC + e] = fmaf(d, n, dw[i * VEC + e]);
-                    db[i * VEC + e] += d;
+                    for (int e = 0; e < VEC; ++e) {
+                        const float d = dy.get(e), n = (x.get(e) - mean[r]) * rstd[r], g = d * w[v * VEC + e];
+                        a += g;
+                        b = fmaf(g, n, b);
+                        dw[v * VEC + e] = fmaf(d, n, dw[v * VEC + e]);
+                        db[v * VEC + e] += d;
+                    }
                 }
             }
-            s[2 * r] = a;
-            s[2 * r + 1] = b;
+            sum[2 * r] = a;
+            sum[2 * r + 1] = b;
         }
-        if (prm.dx) {
-            // part[k] was last read two rounds ago, before the barrier of the round between
+        // lane j of each eight (R = 4) is left with sum j over the warp: each step hands half of the sums over
+        float total[2 * R];
+        {
+            int width = 2 * R;
 #pragma unroll
-            for (int j = 0; j < 2 * R; ++j) s[j] = lanes_sum<32>(s[j]);
-            if (lane == 0) {
+            for (int o = 16; o > 0; o >>= 1) {
+                if (width > 1) {
+                    width /= 2;
+                    const bool up = (lane & o) != 0;
 #pragma unroll
-                for (int j = 0; j < 2 * R; ++j) part[k][warp][j] = s[j];
+                    for (int j = 0; j < R; ++j) {
+                        if (j >= width) continue;
+                        const float keep = up ? sum[j + width] : sum[j], give = up ? sum[j] : sum[j + width];
+                        sum[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+                    }
+                } else {
+                    sum[0] += __shfl_xor_sync(0xffffffffu, sum[0], o);
+                }
             }
-            __syncthreads();
+            // part[k] was last read two rounds ago, before the barrier of the round between
+            constexpr int SHARE = 32 / (2 * R);
+            if (lane % SHARE == 0) part[k][warp][lane / SHARE] = sum[0];
+        }
+        __syncthreads();
+        // every thread is done with the round before: its stage takes the rows of the round that comes after those under way
+        if (threadIdx.x == 0 && i > 0 && i - 1 + stages < rounds) fill(i - 1 + stages);
+        if (prm.dx) {
 #pragma unroll
-            for (int j = 0; j < 2 * R; ++j) s[j] = 0.f;
+            for (int j = 0; j < 2 * R; ++j) total[j] = 0.f;
             for (int q = 0; q < warps; ++q)
 #pragma unroll
-                for (int j = 0; j < 2 * R; ++j) s[j] += part[k][q][j];
+                for (int j = 0; j < 2 * R; j += 2) {
+                    const float2 t = *reinterpret_cast<const float2 *>(&part[k][q][j]);
+                    total[j] += t.x;
+                    total[j + 1] += t.y;
+                }
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                if (r0 + r >= row_end) continue;
-                const float a = s[2 * r] * inv_cols, b = s[2 * r + 1] * inv_cols;
+                if (r >= live) continue;
+                const float a = total[2 * r] * inv_cols, b = total[2 * r + 1] * inv_cols;
 #pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    if (!in[i]) continue;
+                for (int v = 0; v < NV; ++v) {
+                    if (!in[v]) continue;
+                    const int c = (v * (int)blockDim.x + (int)threadIdx.x) * VEC;
+                    Vec<T, VEC> x, dy, o;
+                    x.load(xs[r] + c);
+                    dy.load(ds[r] + c);
                     float f[VEC];
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) {
-                        const float n = (x[r][i].get(e) - mean[r]) * rstd[r];
-                        f[e] = rstd[r] * (dy[r][i].get(e) * weight(i, e) - a - n * b);
+                        const float n = (x.get(e) - mean[r]) * rstd[r];
+                        f[e] = rstd[r] * (dy.get(e) * w[v * VEC + e] - a - n * b);
                     }
-                    Vec<T, VEC> o;
                     o.set(f);
-                    o.store((T *)prm.dx + (r0 + r) * prm.stride_dx + (i * (int)blockDim.x + (int)threadIdx.x) * VEC);
+                    o.store((T *)prm.dx + (r0 + r) * prm.stride_dx + c);
                 }
             }
         }
     }
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (i * (int)blockDim.x + (int)threadIdx.x) * VEC;
-        if (!in[i]) continue;
-        if (prm.partial) {
-            float *p = prm.partial + ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 2 * cols + c;
+    for (int v = 0; v < NV; ++v) {
+        const int c = (v * (int)blockDim.x + (int)threadIdx.x) * VEC;
+        if (!in[v]) continue;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                p[e] = dw[i * VEC + e];
-                p[cols + e] = db[i * VEC + e];
-            }
-        } else {
-            Vec<W, VEC> o;
-            if (prm.dweight) {
-                o.set(dw + i * VEC);
-                o.store((W *)prm.dweight + blockIdx.y * prm.stride_dw + c);
-            }
-            if (prm.dbias) {
-                o.set(db + i * VEC);
-                o.store((W *)prm.dbias + blockIdx.y * prm.stride_dw + c);
-            }
+        for (int e = 0; e < VEC; ++e) {
+            write_sum<W>(prm, 0, c + e, dw[v * VEC + e]);
+            write_sum<W>(prm, 1, c + e, db[v * VEC + e]);
         }
     }
 }
@@ -322,7 +492,7 @@ layer_norm_sums_kernel(const float *partial, void *dweight, void *dbias, int col
     float sum = 0.f;
     if (c < cols) {
         const float *p = partial + ((long long)blockIdx.y * ctas * 2 + which) * cols + c;
-#pragma unroll 4
+#pragma unroll 8
         for (int i = slot; i < ctas; i += SUMS) sum += p[(long long)i * 2 * cols];
     }
     part[slot][lane] = sum;
@@ -412,46 +582,94 @@ int forward_by_cols(const ForwardParams &prm, bool overlap, cudaStream_t stream)
     }
 }
 
-// The backward grid: threads of a CTA, vectors of a thread, rows at a time, CTAs of a group.
+// The backward grid.  lanes > 0: that many lanes have a row; else CTAs of `threads` threads with nv vectors each, r rows
+// at a time and a ring of `stages` rounds of them.
 struct BackwardGrid {
-    int threads, nv, r;
-    long long ctas;
+    int lanes, threads, nv, r, stages, pitch;
+    long long ctas;   // of a group
 };
 
+constexpr int RING_BYTES = 220 << 10;   // shared memory of an SM for the rings of its CTAs
+
 BackwardGrid backward_grid(const Shape &s, int vec, int sms) {
-    BackwardGrid g;
+    BackwardGrid g{};
     const int n = (s.cols + vec - 1) / vec;
-    g.nv = 1;
-    while (n > g.nv * (vec > 1 ? 512 : 1024)) g.nv *= 2;
-    g.threads = ((n + g.nv - 1) / g.nv + 31) / 32 * 32;
-    g.r = g.nv == 1 ? 4 : g.nv == 2 ? 2 : 1;
-    const long long resident = (long long)sms * std::max(1, 1024 / g.threads);
-    const long long most = (s.rows_per_group + g.r - 1) / g.r;   // a round of rows each at least
+    long long resident, most;   // CTAs that run at once; those that have rows
+    if (n <= 32) {
+        g.lanes = n <= 8 ? 8 : 32;
+        g.threads = 256;
+        g.r = 4;
+        resident = (long long)sms * 4;
+        most = (s.rows_per_group + g.r * (256 / g.lanes) - 1) / (g.r * (256 / g.lanes));
+    } else {
+        const int most_nv = 32 / vec;
+        for (g.nv = 1; g.nv < most_nv && n > 256 * g.nv; g.nv *= 2) {
+        }
+        g.threads = std::min(512, ((n + g.nv - 1) / g.nv + 31) / 32 * 32);
+        const int per_sm = std::max(1, std::min(4, 640 / g.threads));
+        // in rows that are not aligned a granule more
+        g.pitch = (int)((s.cols * s.esz + 15) / 16 * 16) + (vec == 1 ? 16 : 0);
+        const int budget = RING_BYTES / per_sm - 2048;   // what the kernel has besides, and the system
+        g.r = g.nv * vec <= 8 ? 4 : g.nv * vec <= 16 ? 2 : 1;
+        while (g.r > 1 && 3 * 2 * g.r * g.pitch > budget) g.r /= 2;
+        g.stages = std::max(1, std::min(MAX_STAGES, budget / (2 * g.r * g.pitch)));
+        resident = (long long)sms * per_sm;
+        most = (s.rows_per_group + g.r - 1) / g.r;
+    }
     g.ctas = std::max(1ll, std::min(most, resident / std::max(1ll, s.groups)));
     return g;
 }
 
 template <class T, class W, int VEC, int NV, int R>
 int launch_backward(const BackwardParams &prm, const BackwardGrid &g, long long groups, bool overlap, cudaStream_t stream) {
-    HB_CUDA(launch_overlapping(layer_norm_bwd_kernel<T, W, VEC, NV, R>, dim3((unsigned)g.ctas, (unsigned)groups), g.threads, 0, 1,
+    const int smem = g.stages * 2 * g.r * g.pitch;
+    // the shared-memory opt-in is an attribute of the kernel on one device
+    static std::atomic<uint64_t> done{0};
+    int dev = -1;
+    HB_CUDA(cudaGetDevice(&dev));
+    if (!(done.load() >> dev & 1)) {
+        HB_CUDA(cudaFuncSetAttribute(layer_norm_bwd_kernel<T, W, VEC, NV, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_BYTES));
+        done.fetch_or(1ull << dev);
+    }
+    HB_CUDA(launch_overlapping(layer_norm_bwd_kernel<T, W, VEC, NV, R>, dim3((unsigned)g.ctas, (unsigned)groups), g.threads, (size_t)smem, 1,
                                stream, overlap, prm));
     HB_LAUNCHED();
     return HILBERTA_OK;
 }
 
+template <class T, class W, int VEC, int LANES>
+int launch_lanes(const BackwardParams &prm, const BackwardGrid &g, long long groups, bool overlap, cudaStream_t stream) {
+    HB_CUDA(launch_overlapping(layer_norm_bwd_lanes_kernel<T, W, VEC, LANES, 4>, dim3((unsigned)g.ctas, (unsigned)groups), 256, 0, 1, stream,
+                               overlap, prm));
+    HB_LAUNCHED();
+    return HILBERTA_OK;
+}
+
+template <class T, class W, int VEC, int NV>
+int backward_by_rows(const BackwardParams &prm, const BackwardGrid &g, long long groups, bool overlap, cudaStream_t stream) {
+    if constexpr (NV * VEC <= 8)
+        if (g.r == 4) return launch_backward<T, W, VEC, NV, 4>(prm, g, groups, overlap, stream);
+    if constexpr (NV * VEC <= 16)
+        if (g.r == 2) return launch_backward<T, W, VEC, NV, 2>(prm, g, groups, overlap, stream);
+    return launch_backward<T, W, VEC, NV, 1>(prm, g, groups, overlap, stream);
+}
+
 template <class T, class W, int VEC>
 int backward_by_cols(const BackwardParams &prm, const BackwardGrid &g, long long groups, bool overlap, cudaStream_t stream) {
+    if (g.lanes == 8) return launch_lanes<T, W, VEC, 8>(prm, g, groups, overlap, stream);
+    if (g.lanes == 32) return launch_lanes<T, W, VEC, 32>(prm, g, groups, overlap, stream);
     switch (g.nv) {
-        case 1: return launch_backward<T, W, VEC, 1, 4>(prm, g, groups, overlap, stream);
-        case 2: return launch_backward<T, W, VEC, 2, 2>(prm, g, groups, overlap, stream);
-        case 4: return launch_backward<T, W, VEC, 4, 1>(prm, g, groups, overlap, stream);
-        case 8:   // 16-bit vectors get by with four
-            if constexpr (VEC < 8) return launch_backward<T, W, VEC, 8, 1>(prm, g, groups, overlap, stream);
-            return HILBERTA_ERR_UNSUPPORTED;
-        default:
-            if constexpr (VEC == 1) return launch_backward<T, W, 1, 16, 1>(prm, g, groups, overlap, stream);
-            return HILBERTA_ERR_UNSUPPORTED;
+        case 1: return backward_by_rows<T, W, VEC, 1>(prm, g, groups, overlap, stream);
+        case 2: return backward_by_rows<T, W, VEC, 2>(prm, g, groups, overlap, stream);
+        case 4: return backward_by_rows<T, W, VEC, 4>(prm, g, groups, overlap, stream);
     }
+    if constexpr (VEC <= 4)
+        if (g.nv == 8) return backward_by_rows<T, W, VEC, 8>(prm, g, groups, overlap, stream);
+    if constexpr (VEC == 1) {
+        if (g.nv == 16) return backward_by_rows<T, W, VEC, 16>(prm, g, groups, overlap, stream);
+        if (g.nv == 32) return backward_by_rows<T, W, VEC, 32>(prm, g, groups, overlap, stream);
+    }
+    return HILBERTA_ERR_UNSUPPORTED;
 }
 
 }  // namespace
@@ -496,10 +714,12 @@ extern "C" size_t hilberta_layer_norm_workspace(int64_t rows, int cols, int64_t 
     if (cudaGetDevice(&dev) != cudaSuccess) return 0;
     const int sms = sm100_count(dev);
     size_t most = 0;
-    for (int vec : {1, 4, 8}) {
-        const BackwardGrid g = backward_grid(s, vec, sms);
-        if (g.ctas > 1) most = std::max(most, (size_t)(g.ctas * s.groups) * 2 * (size_t)cols * sizeof(float));
-    }
+    for (size_t esz : {2, 4})   // whatever the type and the alignment
+        for (int vec : {1, (int)(16 / esz)}) {
+            s.esz = esz;
+            const BackwardGrid g = backward_grid(s, vec, sms);
+            if (g.ctas > 1) most = std::max(most, (size_t)(g.ctas * s.groups) * 2 * (size_t)cols * sizeof(float));
+        }
     return most;
 }
 
@@ -533,12 +753,14 @@ extern "C" int hilberta_layer_norm_backward(const void *dy, const void *x, const
     }
     const bool one = s.groups == 1;
     BackwardParams prm{dy, x, weight, mean, rstd, dx, dweight, dbias, nullptr, rows, s.rows_per_group, stride_dy, stride_x, stride_dx,
-                       one ? 0 : stride_w, one ? 0 : stride_dw, cols, unit_offset ? 1.f : 0.f};
+                       one ? 0 : stride_w, one ? 0 : stride_dw, cols, unit_offset ? 1.f : 0.f, 0, 0};
     const int vec = (int)(16 / s.esz);
     const bool vectors = cols % vec == 0 && aligned16(dy, stride_dy, s.esz) && aligned16(x, stride_x, s.esz) && aligned16(dx, stride_dx, s.esz) &&
                          aligned16(weight, prm.stride_w, s.wsz) && aligned16(dweight, prm.stride_dw, s.wsz) &&
                          aligned16(dbias, prm.stride_dw, s.wsz);
     BackwardGrid g = backward_grid(s, vectors ? vec : 1, sms);
+    prm.stages = g.stages;
+    prm.pitch = g.pitch;
     const bool sums = (dweight || dbias) && g.ctas > 1;
     if (sums) {
         if (!workspace || workspace_bytes < (size_t)(g.ctas * s.groups) * 2 * (size_t)cols * sizeof(float)) return HILBERTA_ERR_BUFFER;

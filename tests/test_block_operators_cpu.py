@@ -109,13 +109,74 @@ def test_rotary_frequencies_refuses(bad):
 
 def test_binding_refuses_shapes_before_the_library():
     x = torch.zeros((2, 3, 8))
-    assert hb._rows(x, "x") == (6, 8) and hb._rows(x[:, :, :4], "x") == (6, 8) and hb._rows(x[:1, :, 2:], "x") == (3, 8)
+    assert hb._row_stride(x, "x") == 8 and hb._row_stride(x[:, :, :4], "x") == 8 and hb._row_stride(x[:1, :, 2:], "x") == 8
     for bad in (x.transpose(0, 2), x[:, :2], x.permute(1, 0, 2)):
         with pytest.raises(ValueError):
-            hb._rows(bad, "x")
+            hb._row_stride(bad, "x")
     with pytest.raises(ValueError):
-        hb._norm_weights(x, (torch.zeros(3, 8),))
-    assert hb._norm_weights(x, (None, None)) == (0, 0, hb.FP32)
-    assert hb._norm_weights(x, (torch.zeros(2, 16)[:, 8:],)) == (3, 16, hb.FP32)
+        hb._norm_weights(x, torch.zeros(3, 8), None)
+    assert hb._norm_weights(x, None, None) == (0, 0, hb.FP32)
+    assert hb._norm_weights(x, torch.zeros(2, 16)[:, 8:], None) == (3, 16, hb.FP32)
     with pytest.raises(ValueError):
-        hb._norm_weights(x, (torch.zeros(8), torch.zeros(8).bfloat16()))
+        hb._norm_weights(x, torch.zeros(8), torch.zeros(8).bfloat16())
+    with pytest.raises(ValueError):
+        hb._norm_weights(x, torch.zeros(2, 8), torch.zeros(2, 16)[:, 8:])
+
+
+def _packed(lib, fn="hilberta_packed_forward", q=1 << 30, k=1 << 31, v=1 << 32, out=1 << 33, lse=None, cu=PTR, n=1, total=10, heads=4, kv=2,
+            dim=64, dtype=hb.BF16, st=(256, 64, 128, 64, 128, 64, 256, 64), scale=0.0):
+    strides = None if st is None else (ctypes.c_int64 * 8)(*st)
+    return lib.hilberta_packed_forward(q, k, v, out, lse, cu, n, total, heads, kv, dim, dtype, strides, 1, scale, None)
+
+
+BAD_PACKED = [
+    (dict(q=None), hb.ERR_INVALID), (dict(k=None), hb.ERR_INVALID), (dict(v=None), hb.ERR_INVALID), (dict(out=None), hb.ERR_INVALID),
+    (dict(cu=None), hb.ERR_INVALID), (dict(st=None), hb.ERR_INVALID), (dict(n=-1), hb.ERR_INVALID), (dict(total=-1), hb.ERR_INVALID),
+    (dict(heads=0), hb.ERR_INVALID), (dict(kv=0), hb.ERR_INVALID), (dict(kv=3), hb.ERR_INVALID), (dict(dim=0), hb.ERR_INVALID),
+    (dict(dim=96), hb.ERR_UNSUPPORTED), (dict(dtype=hb.FP32), hb.ERR_UNSUPPORTED), (dict(dtype=hb.FP8_E4M3), hb.ERR_UNSUPPORTED),
+    (dict(dtype=9), hb.ERR_INVALID), (dict(n=65537), hb.ERR_UNSUPPORTED), (dict(total=(1 << 26) + 1), hb.ERR_UNSUPPORTED),
+    (dict(q=(1 << 30) + 8), hb.ERR_INVALID), (dict(lse=PTR + 1), hb.ERR_INVALID), (dict(cu=PTR + 2), hb.ERR_INVALID),
+    (dict(st=(256, 60, 128, 64, 128, 64, 256, 64)), hb.ERR_INVALID), (dict(st=(256, 64, 0, 64, 128, 64, 256, 64)), hb.ERR_INVALID),
+    (dict(st=(256, 64, 128, 64, -128, 64, 256, 64)), hb.ERR_INVALID), (dict(scale=float("nan")), hb.ERR_INVALID),
+    (dict(out=1 << 30), hb.ERR_INVALID), (dict(out=(1 << 31) + 128), hb.ERR_INVALID),
+]
+
+
+@pytest.mark.parametrize("bad,status", BAD_PACKED)
+def test_packed_forward_refuses(lib, bad, status):
+    assert _packed(lib, **bad) == status
+
+
+def _packed_grad(lib, ptrs=None, lse=PTR, ws=PTR, ws_bytes=320, cu=PTR, n=1, total=10, heads=4, kv=2, dim=64, dtype=hb.BF16, st=None, scale=0.0):
+    p = [(i + 1) << 30 for i in range(8)]
+    for i, x in (ptrs or {}).items():
+        p[i] = x
+    q, k = (256, 64), (128, 64)
+    strides = (ctypes.c_int64 * 16)(*(st or q + q + k + k + q + q + k + k))
+    return lib.hilberta_packed_backward(*p[:5], lse, *p[5:], ws, ws_bytes, cu, n, total, heads, kv, dim, dtype, strides, 1, scale, None)
+
+
+@pytest.mark.parametrize("bad,status", [(dict(ptrs={i: None}), hb.ERR_INVALID) for i in range(8)] + [
+    (dict(lse=None), hb.ERR_INVALID), (dict(ws=None), hb.ERR_BUFFER), (dict(ws_bytes=319), hb.ERR_BUFFER), (dict(ws=PTR + 8), hb.ERR_INVALID),
+    (dict(ptrs={5: 1 << 30}), hb.ERR_INVALID), (dict(ptrs={6: (7 << 30) + 64, 7: 7 << 30}), hb.ERR_INVALID), (dict(kv=3), hb.ERR_INVALID),
+    (dict(dim=32), hb.ERR_UNSUPPORTED), (dict(dtype=hb.FP32), hb.ERR_UNSUPPORTED), (dict(scale=float("nan")), hb.ERR_INVALID),
+])
+def test_packed_backward_refuses(lib, bad, status):
+    assert _packed_grad(lib, **bad) == status
+
+
+def test_slices_of_one_buffer_pass_the_overlap_test(lib):
+    """q, k, v and out side by side within a token, or head by head: accepted up to the point where a device is needed."""
+    if torch.cuda.is_available():
+        pytest.skip("would launch on made-up pointers")
+    base = 1 << 30
+    token = (4 + 2 + 2 + 4) * 64
+    st = (token, 64) * 4
+    ok = _packed(lib, q=base, k=base + 512, v=base + 768, out=base + 1024, st=st)
+    assert ok == hb.ERR_CUDA
+    assert _packed(lib, q=base, k=base + 512, v=base + 768, out=base + 1000 // 16 * 16, st=st) == hb.ERR_INVALID
+    pairs = (1024, 128) * 4   # q and out interleaved head by head, one key head for each
+    far = 1 << 40
+    assert _packed(lib, q=base, k=far, v=far + (1 << 30), out=base + 128, kv=4, st=pairs) == hb.ERR_CUDA
+    assert _packed(lib, q=base, k=far, v=far + (1 << 30), out=base + 112, kv=4, st=pairs) == hb.ERR_INVALID
+    assert lib.hilberta_packed_workspace(10, 4) == 320 and lib.hilberta_packed_workspace(0, 4) == 0
