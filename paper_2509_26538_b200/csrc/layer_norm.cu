@@ -10,6 +10,8 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <atomic>
+#include <type_traits>
 
 #include "common.cuh"
 #include "sm100_ptx.cuh"
@@ -32,6 +34,9 @@ struct Vec {
                 const uint4 v = *(reinterpret_cast<const uint4 *>(p) + i);
                 w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
             }
+        } else if constexpr (BYTES == 8) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(p);
+            w[0] = v.x, w[1] = v.y;
         } else if constexpr (BYTES == 4) {
             w[0] = *reinterpret_cast<const uint32_t *>(p);
         } else {
@@ -45,6 +50,11 @@ struct Vec {
     __device__ __forceinline__ float get(int i) const {
         if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
         else return __uint_as_float((i & 1) ? (w[i >> 1] & 0xffff0000u) : (w[i >> 1] << 16));
+    }
+    // elements 2 i and 2 i + 1; of a single element the second is zero
+    __device__ __forceinline__ float2 pair(int i) const {
+        if constexpr (VEC == 1) return make_float2(get(0), 0.f);
+        else return make_float2(get(2 * i), get(2 * i + 1));
     }
     __device__ __forceinline__ void set(const float *f) {
         if constexpr (sizeof(T) == 4) {
@@ -65,6 +75,8 @@ struct Vec {
 #pragma unroll
             for (int i = 0; i < BYTES / 16; ++i)
                 *(reinterpret_cast<uint4 *>(p) + i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        } else if constexpr (BYTES == 8) {
+            *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
         } else if constexpr (BYTES == 4) {
             *reinterpret_cast<uint32_t *>(p) = w[0];
         } else {
@@ -72,6 +84,12 @@ struct Vec {
         }
     }
 };
+
+// Two elements at a time: Blackwell's packed fp32 instructions, which halve the arithmetic of these kernels (a single
+// element has the other half idle).
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+template <int VEC>
+constexpr int PAIRS = (VEC + 1) / 2;
 
 struct ForwardParams {
     const void *x, *weight, *bias;
@@ -183,18 +201,22 @@ struct BackwardParams {
     long long rows, rows_per_group, stride_dy, stride_x, stride_dx, stride_w, stride_dw;
     int cols;
     float offset;
+    int team_warps;      // warps that share a row
     int stages, pitch;   // of the ring in shared memory
 };
 
 // weights as the gradients use them: w [+ 1], 1 without any
 template <class W, int VEC>
-__device__ __forceinline__ void load_weights(float *w, const W *p, bool given, float offset) {
+__device__ __forceinline__ void load_weights(float2 *w, const W *p, bool given, float offset) {
     Vec<W, VEC> v;
     v.zero();
     if (given) v.load(p);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) w[e] = given ? v.get(e) + offset : 1.f;
+    for (int e = 0; e < PAIRS<VEC>; ++e) w[e] = given ? __fadd2_rn(v.pair(e), both(offset)) : both(1.f);
 }
+
+// (x - mean) rstd: the difference first: with a mean far from zero, x rstd - mean rstd would lose what they share.
+__device__ __forceinline__ float2 normalised(float2 x, float mean, float2 scale) { return __fmul2_rn(__fadd2_rn(x, both(-mean)), scale); }
 
 // this CTA's sum over its rows of dy n (which = 0) or dy (1) for one column: a partial sum, or the result
 template <class W>
@@ -229,7 +251,8 @@ layer_norm_bwd_lanes_kernel(const BackwardParams prm) {
     const long long row_end = min(row_begin + prm.rows_per_group, prm.rows);
     const float inv_cols = 1.f / (float)cols;
     const bool in = c < cols;
-    float dw[VEC] = {}, db[VEC] = {}, w[VEC];
+    constexpr int P = PAIRS<VEC>;
+    float2 dw[P] = {}, db[P] = {}, w[P];
     allow_next();
     wait_for_previous();
     load_weights<W, VEC>(w, (const W *)prm.weight + blockIdx.y * prm.stride_w + c, prm.weight && in, prm.offset);
@@ -252,35 +275,43 @@ layer_norm_bwd_lanes_kernel(const BackwardParams prm) {
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            float n[VEC], g[VEC], a = 0.f, b = 0.f;
+            const float2 scale = both(rstd[r]);
+            float2 n[P], g[P], a2 = both(0.f), b2 = both(0.f);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const float d = dy[r].get(e);
-                n[e] = (x[r].get(e) - mean[r]) * rstd[r];
-                g[e] = d * w[e];
+            for (int e = 0; e < P; ++e) {
+                const float2 d = dy[r].pair(e);
+                n[e] = normalised(x[r].pair(e), mean[r], scale);
+                g[e] = __fmul2_rn(d, w[e]);
                 if (in) {
-                    a += g[e];
-                    b = fmaf(g[e], n[e], b);
-                    dw[e] = fmaf(d, n[e], dw[e]);
-                    db[e] += d;
+                    a2 = __fadd2_rn(a2, g[e]);
+                    b2 = __ffma2_rn(g[e], n[e], b2);
+                    dw[e] = __ffma2_rn(d, n[e], dw[e]);
+                    db[e] = __fadd2_rn(db[e], d);
                 }
             }
-            a = lanes_sum<LANES>(a) * inv_cols;
-            b = lanes_sum<LANES>(b) * inv_cols;
+            const float a = -rstd[r] * (lanes_sum<LANES>(a2.x + a2.y) * inv_cols), b = -rstd[r] * (lanes_sum<LANES>(b2.x + b2.y) * inv_cols);
             if (prm.dx && in && r0 + r < row_end) {
                 Vec<T, VEC> o;
-                float f[VEC];
+                float f[2 * P];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) f[e] = rstd[r] * (g[e] - a - n[e] * b);
+                for (int e = 0; e < P; ++e) {
+                    const float2 d = __ffma2_rn(g[e], scale, __ffma2_rn(n[e], both(b), both(a)));
+                    f[2 * e] = d.x;
+                    f[2 * e + 1] = d.y;
+                }
                 o.set(f);
                 o.store((T *)prm.dx + (r0 + r) * prm.stride_dx + c);
             }
         }
     }
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-        part[0][team][c + e] = dw[e];
-        part[1][team][c + e] = db[e];
+    for (int e = 0; e < P; ++e) {
+        part[0][team][c + 2 * e] = dw[e].x;
+        part[1][team][c + 2 * e] = db[e].x;
+        if (VEC > 1) {
+            part[0][team][c + 2 * e + 1] = dw[e].y;
+            part[1][team][c + 2 * e + 1] = db[e].y;
+        }
     }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * cols; i += 256) {
@@ -292,122 +323,150 @@ layer_norm_bwd_lanes_kernel(const BackwardParams prm) {
     }
 }
 
-// Longer rows: the CTA is the team.  R rows at a time come through a ring of shared memory, filled STAGES - 1 rounds
-// ahead by bulk copies (a register's worth of loads ahead left HBM idle at the barrier that the two row sums need), and
-// are read from there twice, for the sums and for dx.  A row that does not start on a 16-byte boundary is copied from the
-// boundary before to the one behind: the granules are those of its own first and last elements.
-constexpr int MAX_STAGES = 4;
+// Longer rows: a team of `warps` warps has a row, a CTA several teams, R rows each at a time.  They come through a ring of
+// shared memory that a warp of its own fills with bulk copies, rounds ahead (a register's worth of loads ahead left HBM
+// idle at the barrier that the two row sums need; filling from a computing warp cost more than the warp), and are read
+// from there twice, for the sums and for dx.  Rows that lie one
+// behind the other are one copy.  A row that does not start on a 16-byte boundary is copied from the boundary before to the
+// one behind: the granules are those of its own first and last elements.  Columns behind the row's end count as zeros.
+constexpr int MAX_STAGES = 4, MAX_ROWS = 16, MAX_WARPS = 16;
 template <class T, class W, int VEC, int NV, int R>
-__global__ void __launch_bounds__(512)
+__global__ void __launch_bounds__(32 * (MAX_WARPS + 1))
 layer_norm_bwd_kernel(const BackwardParams prm) {
     extern __shared__ __align__(16) uint8_t ring[];
-    __shared__ __align__(16) float part[2][16][2 * R];
-    __shared__ uint64_t full[MAX_STAGES];
-    const int cols = prm.cols, warps = blockDim.x / 32, warp = threadIdx.x / 32, lane = threadIdx.x % 32, stages = prm.stages;
+    __shared__ __align__(16) float part[2][MAX_WARPS][2 * R];
+    __shared__ __align__(16) float2 stats[MAX_STAGES][MAX_ROWS];   // -mean, rstd of a stage's rows
+    __shared__ uint64_t full[MAX_STAGES], empty[MAX_STAGES];
+    constexpr int P = NV * VEC / 2;           // pairs of a thread
+    constexpr bool KEEP_W = NV * VEC <= 16;   // weights in registers, else from the first-level cache
+    const int cols = prm.cols, all = (int)blockDim.x / 32 - 1, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warps = prm.team_warps, teams = all / warps, rows = teams * R;   // rows of a round
+    const int stages = prm.stages, pitch = prm.pitch;                          // pitch: bytes of a row in the ring
     const long long row_begin = (long long)blockIdx.y * prm.rows_per_group;
     const long long row_end = min(row_begin + prm.rows_per_group, prm.rows);
-    const long long first = row_begin + (long long)blockIdx.x * R, step = (long long)gridDim.x * R;
+    const long long first = row_begin + (long long)blockIdx.x * rows, step = (long long)gridDim.x * rows;
     const int rounds = first < row_end ? (int)((row_end - first + step - 1) / step) : 0;
-    const float inv_cols = 1.f / (float)cols;
-    const int pitch = prm.pitch;   // bytes of a row in the ring
-    float dw[NV * VEC] = {}, db[NV * VEC] = {};
-    float w[NV * VEC];
+    const uint32_t full0 = ptx::smem_u32(full), empty0 = ptx::smem_u32(empty);
     if (threadIdx.x == 0) {
-        for (int i = 0; i < stages; ++i) ptx::mbar_init(ptx::smem_u32(&full[i]), 1);
+        for (int i = 0; i < stages; ++i) {
+            ptx::mbar_init(full0 + 8 * i, 1);
+            ptx::mbar_init(empty0 + 8 * i, all);
+        }
         ptx::mbar_fence_init();
     }
     allow_next();
     wait_for_previous();
     __syncthreads();
-    // x and dy of round i into its stage
-    auto fill = [&](int i) {
-        const int s = i % stages;
-        const uint32_t bar = ptx::smem_u32(&full[s]), to = ptx::smem_u32(ring) + (uint32_t)(s * 2 * R * pitch);
-        const long long r0 = first + i * step;
-        const int live = (int)min((long long)R, row_end - r0);
-        const T *src[2] = {(const T *)prm.x + r0 * prm.stride_x, (const T *)prm.dy + r0 * prm.stride_dy};
-        const long long stride[2] = {prm.stride_x, prm.stride_dy};
-        uint32_t bytes = 0;
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-            for (int r = 0; r < live; ++r) {
-                const uintptr_t at = (uintptr_t)(src[k] + r * stride[k]), from = at & ~(uintptr_t)15;
-                bytes += (uint32_t)((at + (size_t)cols * sizeof(T) + 15 & ~(uintptr_t)15) - from);
-            }
-        ptx::mbar_expect_tx(bar, bytes);
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-            for (int r = 0; r < live; ++r) {
-                const uintptr_t at = (uintptr_t)(src[k] + r * stride[k]), from = at & ~(uintptr_t)15;
-                bulk_load(to + (uint32_t)((k * R + r) * pitch), (const void *)from,
-                          (uint32_t)((at + (size_t)cols * sizeof(T) + 15 & ~(uintptr_t)15) - from), bar);
-            }
-    };
-    if (threadIdx.x == 0)
-        for (int i = 0; i < stages && i < rounds; ++i) fill(i);
-    bool in[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (i * (int)blockDim.x + (int)threadIdx.x) * VEC;
-        in[i] = c < cols;
-        load_weights<W, VEC>(w + i * VEC, (const W *)prm.weight + blockIdx.y * prm.stride_w + c, prm.weight && in[i], prm.offset);
+    if (warp == all) {
+        // ------------------------------------------------ fills the ring: x, dy and the statistics of each round's rows
+        // lane r < rows is for row r of x, lane rows + r for row r of dy; where a tensor's rows lie one behind the other
+        // its first lane copies them all
+        const bool of_x = lane < rows;
+        const int r = of_x ? lane : lane - rows;
+        const long long stride = of_x ? prm.stride_x : prm.stride_dy;
+        const bool dense = VEC > 1 && stride == cols;
+        const T *src = (const T *)(of_x ? prm.x : prm.dy) + (first + r) * stride;
+        for (int i = 0; i < rounds; ++i, src += step * stride) {
+            const int s = i % stages;
+            const long long r0 = first + i * step;
+            const int live = (int)min((long long)rows, row_end - r0);
+            const bool mine = r < live;
+            const float value = mine ? (of_x ? prm.mean : prm.rstd)[r0 + r] : 0.f;
+            // bounded, like every wait; the readers' arrivals cannot fail
+            ptx::mbar_wait(empty0 + 8 * s, ((i / stages) & 1) ^ 1);
+            if (r < rows) (of_x ? stats[s][r].x : stats[s][r].y) = of_x ? -value : value;
+            const uintptr_t at = (uintptr_t)src, from = at & ~(uintptr_t)15;
+            uint32_t bytes = mine ? (uint32_t)(((at + (size_t)cols * sizeof(T) + 15) & ~(uintptr_t)15) - from) : 0u;
+            if (dense) bytes = r == 0 ? bytes * live : 0u;
+            const uint32_t sum = __reduce_add_sync(0xffffffffu, bytes);
+            if (lane == 0) ptx::mbar_expect_tx(full0 + 8 * s, sum);
+            __syncwarp();
+            if (bytes) bulk_load(ptx::smem_u32(ring) + (uint32_t)((s * 2 * rows + lane) * pitch), (const void *)from, bytes, full0 + 8 * s);
+        }
     }
-    float mean_ahead[R], rstd_ahead[R];   // of the next round
-    auto statistics = [&](long long r0) {
+    const int team = warp / warps, threads = 32 * warps, tid = (warp - team * warps) * 32 + lane;
+    const W *weight = prm.weight ? (const W *)prm.weight + blockIdx.y * prm.stride_w : nullptr;
+    const float inv_cols = 1.f / (float)cols;
+    float2 dw[P] = {}, db[P] = {}, w[KEEP_W ? P : (VEC > 1 ? VEC / 2 : 1)];
+    // this thread's vector v: its column
+    auto col = [&](int v) { return (v * threads + tid) * VEC; };
+    // pairs of vector v (VEC > 1) or of elements v and v + 1 (VEC = 1), zeros behind the row's end
+    auto load_pairs = [&](float2 *to, const auto *row, int v) {
+        using E = std::remove_cv_t<std::remove_pointer_t<decltype(row)>>;
+        if constexpr (VEC > 1) {
+            Vec<E, VEC> t;
+            t.zero();
+            if (col(v) < cols) t.load(row + col(v));
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            mean_ahead[r] = r0 + r < row_end ? prm.mean[r0 + r] : 0.f;
-            rstd_ahead[r] = r0 + r < row_end ? prm.rstd[r0 + r] : 0.f;
+            for (int e = 0; e < VEC / 2; ++e) to[e] = t.pair(e);
+        } else {
+            Vec<E, 1> t0, t1;
+            t0.zero();
+            t1.zero();
+            if (col(v) < cols) t0.load(row + col(v));
+            if (col(v + 1) < cols) t1.load(row + col(v + 1));
+            to[0] = make_float2(t0.get(0), t1.get(0));
         }
     };
-    statistics(first);
-    for (int i = 0; i < rounds; ++i) {
-        const int s = i % stages, k = i & 1;
-        const long long r0 = first + i * step;
-        const int live = (int)min((long long)R, row_end - r0);
-        float mean[R], rstd[R], sum[2 * R];
+    constexpr int STEP = VEC > 1 ? 1 : 2, PV = VEC > 1 ? VEC / 2 : 1;   // vectors and pairs at a time
+    auto load_w = [&](float2 *to, int v) {
+        if (weight) {
+            load_pairs(to, weight, v);
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            mean[r] = mean_ahead[r];
-            rstd[r] = rstd_ahead[r];
+            for (int e = 0; e < PV; ++e) to[e] = __fadd2_rn(to[e], both(prm.offset));
+        } else {
+#pragma unroll
+            for (int e = 0; e < PV; ++e) to[e] = both(1.f);
         }
-        statistics(r0 + step);
-        const T *xs[R], *ds[R];   // the rows in the ring
+    };
+    if (warp < all && KEEP_W) {
+#pragma unroll
+        for (int v = 0; v < NV; v += STEP) load_w(w + v / STEP * PV, v);
+    }
+    // VEC = 1: where a row starts within its granule
+    const T *x0 = (const T *)prm.x + (first + team * R) * prm.stride_x, *dy0 = (const T *)prm.dy + (first + team * R) * prm.stride_dy;
+    T *dx = prm.dx ? (T *)prm.dx + (first + team * R) * prm.stride_dx : nullptr;
+    const uint8_t *const mine = ring + team * R * pitch;
+    const int to_dy = rows * pitch;
+    int s = 0, phase = 0;
+    for (int i = 0; warp < all && i < rounds; ++i) {
+        const int left = (int)min((long long)R, row_end - first - i * step - team * R);   // rows of the team in this round
+        const uint8_t *const base = mine + s * 2 * to_dy;
+        auto row_x = [&](int r) { return (const T *)(base + r * pitch + (VEC == 1 ? (int)((uintptr_t)(x0 + r * prm.stride_x) & 15) : 0)); };
+        auto row_dy = [&](int r) { return (const T *)(base + to_dy + r * pitch + (VEC == 1 ? (int)((uintptr_t)(dy0 + r * prm.stride_dy) & 15) : 0)); };
+        ptx::mbar_wait(full0 + 8 * s, phase);
+        float2 st[R];
+        float sum[2 * R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const uint8_t *base = ring + (size_t)s * 2 * R * pitch;
-            // VEC = 1: the offset within the granule
-            xs[r] = (const T *)(base + r * pitch + (VEC == 1 ? ((uintptr_t)((const T *)prm.x + (r0 + r) * prm.stride_x) & 15) : 0));
-            ds[r] = (const T *)(base + (R + r) * pitch + (VEC == 1 ? ((uintptr_t)((const T *)prm.dy + (r0 + r) * prm.stride_dy) & 15) : 0));
-        }
-        if (!ptx::mbar_wait(ptx::smem_u32(&full[s]), (i / stages) & 1)) return;   // never: the copy's bytes have been asked for
+            float2 a = both(0.f), b = both(0.f);
+            st[r] = stats[s][team * R + r];
+            if (r < left) {
+                const float2 shift = both(st[r].x), scale = both(st[r].y);
+                const T *px = row_x(r), *pd = row_dy(r);
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float a = 0.f, b = 0.f;
-            if (r < live) {
+                for (int v = 0; v < NV; v += STEP) {
+                    float2 x[PV], dy[PV];
+                    float2 *const wv = KEEP_W ? w + v / STEP * PV : w;
+                    if (!KEEP_W) load_w(wv, v);
+                    load_pairs(x, px, v);
+                    load_pairs(dy, pd, v);
 #pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    if (!in[v]) continue;
-                    const int c = (v * (int)blockDim.x + (int)threadIdx.x) * VEC;
-                    Vec<T, VEC> x, dy;
-                    x.load(xs[r] + c);
-                    dy.load(ds[r] + c);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const float d = dy.get(e), n = (x.get(e) - mean[r]) * rstd[r], g = d * w[v * VEC + e];
-                        a += g;
-                        b = fmaf(g, n, b);
-                        dw[v * VEC + e] = fmaf(d, n, dw[v * VEC + e]);
-                        db[v * VEC + e] += d;
+                    for (int e = 0; e < PV; ++e) {
+                        const int at = v / STEP * PV + e;
+                        const float2 n = __fmul2_rn(__fadd2_rn(x[e], shift), scale), g = __fmul2_rn(dy[e], wv[e]);
+                        a = __fadd2_rn(a, g);
+                        b = __ffma2_rn(g, n, b);
+                        dw[at] = __ffma2_rn(dy[e], n, dw[at]);
+                        db[at] = __fadd2_rn(db[at], dy[e]);
                     }
                 }
             }
-            sum[2 * r] = a;
-            sum[2 * r + 1] = b;
+            sum[2 * r] = a.x + a.y;
+            sum[2 * r + 1] = b.x + b.y;
         }
-        // lane j of each eight (R = 4) is left with sum j over the warp: each step hands half of the sums over
-        float total[2 * R];
-        {
+        if (dx) {
+            // lane 32 j / (2 R) is left with sum j over the warp: each step hands half of the sums over
             int width = 2 * R;
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) {
@@ -424,61 +483,92 @@ layer_norm_bwd_kernel(const BackwardParams prm) {
                     sum[0] += __shfl_xor_sync(0xffffffffu, sum[0], o);
                 }
             }
-            // part[k] was last read two rounds ago, before the barrier of the round between
             constexpr int SHARE = 32 / (2 * R);
+            // part[k] was last read two rounds ago, before the barrier of the round between
+            const int k = i & 1;
             if (lane % SHARE == 0) part[k][warp][lane / SHARE] = sum[0];
-        }
-        __syncthreads();
-        // every thread is done with the round before: its stage takes the rows of the round that comes after those under way
-        if (threadIdx.x == 0 && i > 0 && i - 1 + stages < rounds) fill(i - 1 + stages);
-        if (prm.dx) {
+            if (warps == 1) __syncwarp();
+            else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(threads) : "memory");   // the team
+            float2 total[R];
 #pragma unroll
-            for (int j = 0; j < 2 * R; ++j) total[j] = 0.f;
+            for (int r = 0; r < R; ++r) total[r] = both(0.f);
             for (int q = 0; q < warps; ++q)
 #pragma unroll
-                for (int j = 0; j < 2 * R; j += 2) {
-                    const float2 t = *reinterpret_cast<const float2 *>(&part[k][q][j]);
-                    total[j] += t.x;
-                    total[j + 1] += t.y;
-                }
+                for (int r = 0; r < R; ++r)
+                    total[r] = __fadd2_rn(total[r], *reinterpret_cast<const float2 *>(&part[k][team * warps + q][2 * r]));
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                if (r >= live) continue;
-                const float a = total[2 * r] * inv_cols, b = total[2 * r + 1] * inv_cols;
+                if (r >= left) continue;
+                // rstd (g - a - n b), n = (x - mean) rstd
+                const float2 shift = both(st[r].x), scale = both(st[r].y);
+                const float2 a = both(-st[r].y * (total[r].x * inv_cols)), b = both(-st[r].y * st[r].y * (total[r].y * inv_cols));
+                const T *px = row_x(r), *pd = row_dy(r);
+                T *const out = dx + r * prm.stride_dx;
 #pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    if (!in[v]) continue;
-                    const int c = (v * (int)blockDim.x + (int)threadIdx.x) * VEC;
-                    Vec<T, VEC> x, dy, o;
-                    x.load(xs[r] + c);
-                    dy.load(ds[r] + c);
-                    float f[VEC];
+                for (int v = 0; v < NV; v += STEP) {
+                    float2 x[PV], dy[PV];
+                    float f[2 * PV];
+                    float2 *const wv = KEEP_W ? w + v / STEP * PV : w;
+                    if (!KEEP_W) load_w(wv, v);
+                    load_pairs(x, px, v);
+                    load_pairs(dy, pd, v);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const float n = (x.get(e) - mean[r]) * rstd[r];
-                        f[e] = rstd[r] * (dy.get(e) * w[v * VEC + e] - a - n * b);
+                    for (int e = 0; e < PV; ++e) {
+                        const float2 d = __ffma2_rn(__fmul2_rn(dy[e], wv[e]), scale, __ffma2_rn(__fadd2_rn(x[e], shift), b, a));
+                        f[2 * e] = d.x;
+                        f[2 * e + 1] = d.y;
                     }
+                    Vec<T, VEC> o;
                     o.set(f);
-                    o.store((T *)prm.dx + (r0 + r) * prm.stride_dx + c);
+                    if (col(v) < cols) o.store(out + col(v));
+                    if (VEC == 1 && col(v + 1) < cols) {
+                        o.set(f + 1);
+                        o.store(out + col(v + 1));
+                    }
                 }
+            }
+            dx += step * prm.stride_dx;
+        }
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(empty0 + 8 * s);
+        if (++s == stages) s = 0, phase ^= 1;
+        x0 += step * prm.stride_x;
+        dy0 += step * prm.stride_dy;
+    }
+    if (!prm.dweight && !prm.dbias) return;
+    // the teams' sums one after the other through the ring, team 0 first: the order is always the same
+    float2 *const sums = reinterpret_cast<float2 *>(ring);   // [pair][thread], dw then db: they fit (see the host)
+    for (int t = 1; t < teams; ++t) {
+        __syncthreads();
+        if (team == t) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) sums[p * threads + tid] = dw[p], sums[(P + p) * threads + tid] = db[p];
+        }
+        __syncthreads();
+        if (team == 0) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                dw[p] = __fadd2_rn(dw[p], sums[p * threads + tid]);
+                db[p] = __fadd2_rn(db[p], sums[(P + p) * threads + tid]);
             }
         }
     }
+    if (team != 0) return;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int c = (v * (int)blockDim.x + (int)threadIdx.x) * VEC;
-        if (!in[v]) continue;
+    for (int v = 0; v < NV; v += STEP) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            write_sum<W>(prm, 0, c + e, dw[v * VEC + e]);
-            write_sum<W>(prm, 1, c + e, db[v * VEC + e]);
+        for (int e = 0; e < PV; ++e) {
+            const float2 a = dw[v / STEP * PV + e], b = db[v / STEP * PV + e];
+            const int c0 = VEC > 1 ? col(v) + 2 * e : col(v), c1 = VEC > 1 ? c0 + 1 : col(v + 1);
+            if (c0 < cols) write_sum<W>(prm, 0, c0, a.x), write_sum<W>(prm, 1, c0, b.x);
+            if (c1 < cols) write_sum<W>(prm, 0, c1, a.y), write_sum<W>(prm, 1, c1, b.y);
         }
     }
 }
 
 // dw, db of a group: the sums of its CTAs added up in a fixed order.  32 columns a block; SUMS rows of threads
 // share the CTAs out.
-constexpr int SUMS = 16;
+constexpr int SUMS = 32;
 template <class W>
 __global__ void __launch_bounds__(32 * SUMS)
 layer_norm_sums_kernel(const float *partial, void *dweight, void *dbias, int cols, int ctas, long long stride_dw) {
@@ -582,94 +672,163 @@ int forward_by_cols(const ForwardParams &prm, bool overlap, cudaStream_t stream)
     }
 }
 
-// The backward grid.  lanes > 0: that many lanes have a row; else CTAs of `threads` threads with nv vectors each, r rows
-// at a time and a ring of `stages` rounds of them.
-struct BackwardGrid {
-    int lanes, threads, nv, r, stages, pitch;
-    long long ctas;   // of a group
+constexpr int MAX_PER_SM = 8;   // CTAs of the backward kernels on one SM
+
+// How the backward pass is cut up.  lanes > 0: that many lanes have a row; else teams of `warps` warps, `each` columns a
+// thread and r rows at a time.
+struct BackwardShape {
+    int lanes, warps, teams, each, vec, r, pitch;
+    long long round() const { return lanes ? (long long)r * (256 / lanes) : (long long)r * teams; }   // rows of a round
 };
 
-constexpr int RING_BYTES = 220 << 10;   // shared memory of an SM for the rings of its CTAs
-
-BackwardGrid backward_grid(const Shape &s, int vec, int sms) {
-    BackwardGrid g{};
-    const int n = (s.cols + vec - 1) / vec;
-    long long resident, most;   // CTAs that run at once; those that have rows
-    if (n <= 32) {
-        g.lanes = n <= 8 ? 8 : 32;
-        g.threads = 256;
+BackwardShape backward_shape(const Shape &s, bool aligned) {
+    BackwardShape g{};
+    if (s.cols <= 256 && (aligned || s.cols <= 32)) {
+        g.lanes = s.cols <= 8 * 8 && aligned ? 8 : 32;
         g.r = 4;
-        resident = (long long)sms * 4;
-        most = (s.rows_per_group + g.r * (256 / g.lanes) - 1) / (g.r * (256 / g.lanes));
-    } else {
-        const int most_nv = 32 / vec;
-        for (g.nv = 1; g.nv < most_nv && n > 256 * g.nv; g.nv *= 2) {
-        }
-        g.threads = std::min(512, ((n + g.nv - 1) / g.nv + 31) / 32 * 32);
-        const int per_sm = std::max(1, std::min(4, 640 / g.threads));
-        // in rows that are not aligned a granule more
-        g.pitch = (int)((s.cols * s.esz + 15) / 16 * 16) + (vec == 1 ? 16 : 0);
-        const int budget = RING_BYTES / per_sm - 2048;   // what the kernel has besides, and the system
-        g.r = g.nv * vec <= 8 ? 4 : g.nv * vec <= 16 ? 2 : 1;
-        while (g.r > 1 && 3 * 2 * g.r * g.pitch > budget) g.r /= 2;
-        g.stages = std::max(1, std::min(MAX_STAGES, budget / (2 * g.r * g.pitch)));
-        resident = (long long)sms * per_sm;
-        most = (s.rows_per_group + g.r - 1) / g.r;
+        return g;
     }
-    g.ctas = std::max(1ll, std::min(most, resident / std::max(1ll, s.groups)));
+    // Columns of a thread: with 16-byte vectors multiples of 8 (4 in fp32), with 8-byte ones of 4.  The fewest idle slots,
+    // then the fewest columns, 8 at least.
+    long long best = -1;
+    const int full = aligned ? (int)(16 / s.esz) : 1;
+    const int most = s.cols > MAX_WARPS * 32 * 16 ? 32 : 16;
+    for (int warps = MAX_WARPS; warps >= 1; --warps)
+        for (int vec = full; vec >= std::min(full, 4); vec /= 2) {
+            const int unit = std::max(vec, 4), each = (s.cols + 32 * warps * unit - 1) / (32 * warps * unit) * unit;
+            if (each > most || (each < 8 && s.cols >= 8 * 32)) continue;
+            const long long cost = (long long)each * 32 * warps;
+            if (best < 0 || cost < best) {
+                best = cost;
+                g.warps = warps;
+                g.each = each;
+                g.vec = vec;
+            }
+        }
+    g.r = g.each <= 8 ? 4 : g.each <= 16 ? 2 : 1;
+    g.pitch = (int)((s.cols * s.esz + 15) / 16 * 16) + (aligned ? 0 : 16);
+    // Teams: eight computing warps a CTA, sixteen where elements come one by one (40000 x 1024 bf16, us: 1 team of 4 warps 50.2,
+    // 2 teams 47.9; 30000 x 1001 bf16 2 teams 93, 4 teams 62.8), but one team of an odd number of warps (36864 x 1152 bf16: 3 warps
+    // 58.8, twice 3 71.6).
+    g.teams = g.warps & (g.warps - 1) ? 1 : std::max(1, std::min((aligned ? 8 : 16) / g.warps, MAX_ROWS / g.r));
+    // Three rounds of the ring in half of an SM, in all of it for a CTA that fills the SM anyway (12000 x 4096 fp32, us: 2 CTAs of
+    // one row at a time 118, 1 CTA of two rows 98).
+    const int limit = (g.warps == MAX_WARPS ? 200 : 110) << 10;
+    while (g.r > 1 && 3 * 2 * g.r * g.teams * g.pitch > limit) g.r /= 2;
+    while (g.teams > 1 && 3 * 2 * g.r * g.teams * g.pitch > limit) --g.teams;
     return g;
 }
 
-template <class T, class W, int VEC, int NV, int R>
-int launch_backward(const BackwardParams &prm, const BackwardGrid &g, long long groups, bool overlap, cudaStream_t stream) {
-    const int smem = g.stages * 2 * g.r * g.pitch;
-    // the shared-memory opt-in is an attribute of the kernel on one device
-    static std::atomic<uint64_t> done{0};
-    int dev = -1;
-    HB_CUDA(cudaGetDevice(&dev));
-    if (!(done.load() >> dev & 1)) {
-        HB_CUDA(cudaFuncSetAttribute(layer_norm_bwd_kernel<T, W, VEC, NV, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_BYTES));
-        done.fetch_or(1ull << dev);
+// A call on its way: what the launchers below need and find out.
+struct BackwardCall {
+    BackwardParams prm;
+    BackwardShape g;
+    long long groups, rows_per_group;
+    bool overlap, sums;        // sums: dweight or dbias are wanted
+    void *workspace;
+    size_t workspace_bytes;
+    int device, sms;
+    cudaStream_t stream;
+    long long ctas;            // of a group
+};
+
+// As many CTAs as run at once, shared out over the groups, none without a round of rows.
+int place(BackwardCall &c, int per_sm) {
+    const long long most = (c.rows_per_group + c.g.round() - 1) / c.g.round();
+    c.ctas = std::max(1ll, std::min(most, (long long)c.sms * std::min(per_sm, MAX_PER_SM) / std::max(1ll, c.groups)));
+    c.sums = c.sums && c.ctas > 1;
+    if (c.sums) {
+        if (!c.workspace || c.workspace_bytes < (size_t)(c.ctas * c.groups) * 2 * (size_t)c.prm.cols * sizeof(float)) return HILBERTA_ERR_BUFFER;
+        c.prm.partial = (float *)c.workspace;
     }
-    HB_CUDA(launch_overlapping(layer_norm_bwd_kernel<T, W, VEC, NV, R>, dim3((unsigned)g.ctas, (unsigned)groups), g.threads, (size_t)smem, 1,
-                               stream, overlap, prm));
+    return HILBERTA_OK;
+}
+
+template <class T, class W, int VEC, int NV, int R>
+int launch_backward(BackwardCall &c) {
+    const BackwardShape &g = c.g;
+    const auto kernel = layer_norm_bwd_kernel<T, W, VEC, NV, R>;
+    // the shared-memory opt-in is an attribute of the kernel on one device
+    static std::atomic<uint64_t> opted{0};
+    if (!(opted.load() >> c.device & 1)) {
+        HB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 << 10));
+        HB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 100));
+        opted.fetch_or(1ull << c.device);
+    }
+    const int threads = 32 * (g.warps * g.teams + 1), stage = 2 * g.r * g.teams * g.pitch;
+    // rows, and afterwards the sums of a team: NV VEC columns, dw and db, of each of its threads
+    const int least = g.teams > 1 ? NV * VEC * 8 * 32 * g.warps : 0;
+    auto ring = [&](int stages) { return std::max(stages * stage, least); };
+    // As many CTAs as run at once with three rounds each (the driver's count, asked once for each shape in turn), then
+    // more rounds if that costs none.
+    static std::atomic<uint64_t> asked{0};   // threads, stage, stages and CTAs of the last answer
+    const uint64_t key = (uint64_t)threads << 40 | (uint64_t)stage << 8;
+    uint64_t known = asked.load();
+    if ((known & ~0xffull) != key) {
+        int stages = std::min(3, std::max(1, (220 << 10) / stage)), per_sm = 0, more = 0;
+        HB_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, (size_t)ring(stages)));
+        if (stages == 3 && ring(4) <= 220 << 10) {
+            HB_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&more, kernel, threads, (size_t)ring(4)));
+            if (more >= per_sm) stages = 4;
+        }
+        known = key | (uint64_t)stages << 4 | (uint64_t)std::max(1, std::min(per_sm, MAX_PER_SM));
+        asked.store(known);
+    }
+    const int stages = (int)(known >> 4 & 15), per_sm = (int)(known & 15);
+    c.prm.stages = stages;
+    const int rc = place(c, per_sm);
+    if (rc != HILBERTA_OK) return rc;
+    HB_CUDA(launch_overlapping(kernel, dim3((unsigned)c.ctas, (unsigned)c.groups), threads, (size_t)ring(stages), 1, c.stream, c.overlap, c.prm));
     HB_LAUNCHED();
     return HILBERTA_OK;
 }
 
 template <class T, class W, int VEC, int LANES>
-int launch_lanes(const BackwardParams &prm, const BackwardGrid &g, long long groups, bool overlap, cudaStream_t stream) {
-    HB_CUDA(launch_overlapping(layer_norm_bwd_lanes_kernel<T, W, VEC, LANES, 4>, dim3((unsigned)g.ctas, (unsigned)groups), 256, 0, 1, stream,
-                               overlap, prm));
+int launch_lanes(BackwardCall &c) {
+    const int rc = place(c, 4);
+    if (rc != HILBERTA_OK) return rc;
+    HB_CUDA(launch_overlapping(layer_norm_bwd_lanes_kernel<T, W, VEC, LANES, 4>, dim3((unsigned)c.ctas, (unsigned)c.groups), 256, 0, 1, c.stream,
+                               c.overlap, c.prm));
     HB_LAUNCHED();
     return HILBERTA_OK;
 }
 
-template <class T, class W, int VEC, int NV>
-int backward_by_rows(const BackwardParams &prm, const BackwardGrid &g, long long groups, bool overlap, cudaStream_t stream) {
-    if constexpr (NV * VEC <= 8)
-        if (g.r == 4) return launch_backward<T, W, VEC, NV, 4>(prm, g, groups, overlap, stream);
-    if constexpr (NV * VEC <= 16)
-        if (g.r == 2) return launch_backward<T, W, VEC, NV, 2>(prm, g, groups, overlap, stream);
-    return launch_backward<T, W, VEC, NV, 1>(prm, g, groups, overlap, stream);
+template <class T, class W, int VEC, int EACH>
+int backward_by_rows(BackwardCall &c) {
+    constexpr int NV = EACH / VEC;
+    if constexpr (EACH <= 8)
+        if (c.g.r == 4) return launch_backward<T, W, VEC, NV, 4>(c);
+    if constexpr (EACH <= 16)
+        if (c.g.r == 2) return launch_backward<T, W, VEC, NV, 2>(c);
+    return launch_backward<T, W, VEC, NV, 1>(c);
 }
 
 template <class T, class W, int VEC>
-int backward_by_cols(const BackwardParams &prm, const BackwardGrid &g, long long groups, bool overlap, cudaStream_t stream) {
-    if (g.lanes == 8) return launch_lanes<T, W, VEC, 8>(prm, g, groups, overlap, stream);
-    if (g.lanes == 32) return launch_lanes<T, W, VEC, 32>(prm, g, groups, overlap, stream);
-    switch (g.nv) {
-        case 1: return backward_by_rows<T, W, VEC, 1>(prm, g, groups, overlap, stream);
-        case 2: return backward_by_rows<T, W, VEC, 2>(prm, g, groups, overlap, stream);
-        case 4: return backward_by_rows<T, W, VEC, 4>(prm, g, groups, overlap, stream);
+int backward_by_each(BackwardCall &c) {
+    switch (c.g.each) {
+        case 8: return backward_by_rows<T, W, VEC, 8>(c);
+        case 16: return backward_by_rows<T, W, VEC, 16>(c);
+        case 24: return backward_by_rows<T, W, VEC, 24>(c);
+        case 32: return backward_by_rows<T, W, VEC, 32>(c);
     }
-    if constexpr (VEC <= 4)
-        if (g.nv == 8) return backward_by_rows<T, W, VEC, 8>(prm, g, groups, overlap, stream);
-    if constexpr (VEC == 1) {
-        if (g.nv == 16) return backward_by_rows<T, W, VEC, 16>(prm, g, groups, overlap, stream);
-        if (g.nv == 32) return backward_by_rows<T, W, VEC, 32>(prm, g, groups, overlap, stream);
+    if constexpr (VEC <= 4) {
+        switch (c.g.each) {
+            case 4: return backward_by_rows<T, W, VEC, 4>(c);
+            case 12: return backward_by_rows<T, W, VEC, 12>(c);
+            case 20: return backward_by_rows<T, W, VEC, 20>(c);
+            case 28: return backward_by_rows<T, W, VEC, 28>(c);
+        }
     }
     return HILBERTA_ERR_UNSUPPORTED;
+}
+
+template <class T, class W>
+int backward_by_cols(BackwardCall &c, bool aligned) {
+    if (c.g.lanes == 8) return launch_lanes<T, W, 8, 8>(c);
+    if (c.g.lanes) return aligned ? launch_lanes<T, W, 8, 32>(c) : launch_lanes<T, W, 1, 32>(c);
+    if constexpr (sizeof(T) == 2)
+        if (c.g.vec == 8) return backward_by_each<T, W, 8>(c);
+    return c.g.vec == 4 ? backward_by_each<T, W, 4>(c) : backward_by_each<T, W, 1>(c);
 }
 
 }  // namespace
@@ -713,14 +872,14 @@ extern "C" size_t hilberta_layer_norm_workspace(int64_t rows, int cols, int64_t 
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess) return 0;
     const int sms = sm100_count(dev);
-    size_t most = 0;
+    long long ctas = 0;
     for (size_t esz : {2, 4})   // whatever the type and the alignment
-        for (int vec : {1, (int)(16 / esz)}) {
+        for (bool aligned : {false, true}) {
             s.esz = esz;
-            const BackwardGrid g = backward_grid(s, vec, sms);
-            if (g.ctas > 1) most = std::max(most, (size_t)(g.ctas * s.groups) * 2 * (size_t)cols * sizeof(float));
+            const BackwardShape g = backward_shape(s, aligned);
+            ctas = std::max(ctas, std::min((s.rows_per_group + g.round() - 1) / g.round(), (long long)sms * MAX_PER_SM / std::max(1ll, s.groups)));
         }
-    return most;
+    return ctas > 1 ? (size_t)(ctas * s.groups) * 2 * (size_t)cols * sizeof(float) : 0;
 }
 
 extern "C" int hilberta_layer_norm_backward(const void *dy, const void *x, const void *weight, const float *mean,
@@ -753,28 +912,32 @@ extern "C" int hilberta_layer_norm_backward(const void *dy, const void *x, const
     }
     const bool one = s.groups == 1;
     BackwardParams prm{dy, x, weight, mean, rstd, dx, dweight, dbias, nullptr, rows, s.rows_per_group, stride_dy, stride_x, stride_dx,
-                       one ? 0 : stride_w, one ? 0 : stride_dw, cols, unit_offset ? 1.f : 0.f, 0, 0};
-    const int vec = (int)(16 / s.esz);
-    const bool vectors = cols % vec == 0 && aligned16(dy, stride_dy, s.esz) && aligned16(x, stride_x, s.esz) && aligned16(dx, stride_dx, s.esz) &&
+                       one ? 0 : stride_w, one ? 0 : stride_dw, cols, unit_offset ? 1.f : 0.f, 0, 0, 0};
+    // rows on 16-byte boundaries, in whole groups of eight columns
+    const bool vectors = cols % 8 == 0 && aligned16(dy, stride_dy, s.esz) && aligned16(x, stride_x, s.esz) && aligned16(dx, stride_dx, s.esz) &&
                          aligned16(weight, prm.stride_w, s.wsz) && aligned16(dweight, prm.stride_dw, s.wsz) &&
                          aligned16(dbias, prm.stride_dw, s.wsz);
-    BackwardGrid g = backward_grid(s, vectors ? vec : 1, sms);
-    prm.stages = g.stages;
-    prm.pitch = g.pitch;
-    const bool sums = (dweight || dbias) && g.ctas > 1;
-    if (sums) {
-        if (!workspace || workspace_bytes < (size_t)(g.ctas * s.groups) * 2 * (size_t)cols * sizeof(float)) return HILBERTA_ERR_BUFFER;
-        prm.partial = (float *)workspace;
-    }
-    const bool overlap = rows * (long long)cols * (long long)s.esz <= kOverlapBytes;
+    BackwardCall c{};
+    c.g = backward_shape(s, vectors);
+    prm.team_warps = c.g.warps;
+    prm.pitch = c.g.pitch;
+    c.prm = prm;
+    c.groups = s.groups;
+    c.rows_per_group = s.rows_per_group;
+    c.overlap = rows * (long long)cols * (long long)s.esz <= (long long)kOverlapBytes;
+    c.sums = dweight || dbias;
+    c.workspace = workspace;
+    c.workspace_bytes = workspace_bytes;
+    c.device = dev;
+    c.sms = sms;
+    c.stream = st;
     return by_types(s, [&](auto t, auto w) {
         using T = decltype(t);
         using W = decltype(w);
-        const int rc2 = vectors ? backward_by_cols<T, W, 16 / (int)sizeof(T)>(prm, g, s.groups, overlap, st)
-                                : backward_by_cols<T, W, 1>(prm, g, s.groups, overlap, st);
-        if (rc2 != HILBERTA_OK || !sums) return rc2;
+        const int rc2 = backward_by_cols<T, W>(c, vectors);
+        if (rc2 != HILBERTA_OK || !c.sums) return rc2;
         HB_CUDA(launch_overlapping(layer_norm_sums_kernel<W>, dim3((unsigned)((cols + 31) / 32), (unsigned)s.groups, 2), 32 * SUMS, 0, 1, st,
-                                   true, (const float *)prm.partial, prm.dweight, prm.dbias, cols, (int)g.ctas, (long long)prm.stride_dw));
+                                   true, (const float *)c.prm.partial, dweight, dbias, cols, (int)c.ctas, (long long)prm.stride_dw));
         HB_LAUNCHED();
         return HILBERTA_OK;
     });
