@@ -37,20 +37,40 @@ struct Params {
     unsigned char axis[MAX_PAIRS];
 };
 
-// cos and sin of pos * turns
-__device__ __forceinline__ float2 cos_sin(int pos, unsigned long long turns) {
-    const unsigned long long u = (unsigned long long)(long long)pos * turns;
-    const unsigned q = (unsigned)((u + (1ull << 61)) >> 62);
-    const int r = (int)((long long)(u - ((unsigned long long)q << 62)) >> 32);   // in [-2^29, 2^29): 2^32 a turn
-    float s, c;
-    sincospif((float)r * (1.f / 2147483648.f), &s, &c);
-    if (q & 1) {
-        const float t = c;
-        c = -s;
-        s = t;
-    }
-    if (q & 2) c = -c, s = -s;
-    return make_float2(c, s);
+// The angle pos * turns as a quarter turn 0 ... 3 and a remainder of at most an eighth of a turn, 2^32 to a turn.  The low
+// half of the 64-bit product is dropped (2^-32 of a turn).
+__device__ __forceinline__ int remainder_of(int pos, unsigned long long turns, unsigned &quarter) {
+    const unsigned lo = (unsigned)turns, hi = (unsigned)(turns >> 32);
+    const unsigned u = __umulhi((unsigned)pos, lo) + (unsigned)pos * hi - (pos < 0 ? lo : 0u);
+    quarter = (u + (1u << 29)) >> 30;
+    return (int)(u - (quarter << 30));
+}
+
+// cos and sin of two angles by their Taylor series, |angle| <= pi / 4: the first terms left out are below 2^-32 and 2^-29 of
+// the result.  Packed arithmetic: two angles an instruction (the library's sincospif for each, 3.2 million angles and no more
+// than one head to use them, took 14.5 us in all).
+__device__ __forceinline__ void cos_sin2(const int *pos, const unsigned long long *turns, float2 &cos, float2 &sin) {
+    unsigned q0, q1;
+    const int r0 = remainder_of(pos[0], turns[0], q0), r1 = remainder_of(pos[1], turns[1], q1);
+    const float unit = 1.4629180792671596e-9f;   // 2 pi / 2^32
+    const float2 x = __fmul2_rn(make_float2((float)r0, (float)r1), make_float2(unit, unit)), z = __fmul2_rn(x, x);
+    auto c2 = [](float v) { return make_float2(v, v); };
+    float2 s = __ffma2_rn(z, c2(1.f / 362880.f), c2(-1.f / 5040.f));
+    s = __ffma2_rn(s, z, c2(1.f / 120.f));
+    s = __ffma2_rn(s, z, c2(-1.f / 6.f));
+    s = __ffma2_rn(__fmul2_rn(s, z), x, x);
+    float2 c = __ffma2_rn(z, c2(-1.f / 3628800.f), c2(1.f / 40320.f));
+    c = __ffma2_rn(c, z, c2(-1.f / 720.f));
+    c = __ffma2_rn(c, z, c2(1.f / 24.f));
+    c = __ffma2_rn(c, z, c2(-0.5f));
+    c = __ffma2_rn(c, z, c2(1.f));
+    auto turn = [](unsigned q, float c, float s, float &co, float &si) {
+        const float a = q & 1 ? s : c, b = q & 1 ? c : s;   // |cos|, |sin|
+        co = __uint_as_float(__float_as_uint(a) ^ (((q + 1) & 2) << 30));
+        si = __uint_as_float(__float_as_uint(b) ^ ((q & 2) << 30));
+    };
+    turn(q0, c.x, s.x, cos.x, sin.x);
+    turn(q1, c.y, s.y, cos.y, sin.y);
 }
 
 template <class T>
@@ -76,6 +96,20 @@ struct Chunk {   // 16 bytes
     }
 };
 
+// The frequencies, from the parameters (where lanes that want different ones are served one after the other) to shared
+// memory once a block.
+struct Table {
+    unsigned long long turns[MAX_PAIRS + 8];
+    int axis[MAX_PAIRS + 8];
+};
+__device__ __forceinline__ void fill_table(Table &t, const Params &p) {
+    for (int i = threadIdx.x; i < p.pairs; i += THREADS) {
+        t.turns[i] = p.turns[i];
+        t.axis[i] = p.axis[i];
+    }
+    __syncthreads();
+}
+
 // Where a thread's tokens lie.
 struct Token {
     long long x, out, pos;   // offsets of head 0 and of the positions
@@ -88,6 +122,33 @@ __device__ __forceinline__ Token locate(const Params &p, long long token, const 
     return {b * p.xb + from * p.xs, b * p.ob + s * p.os, (b * p.pos_stride_b + at) * p.axes, at};
 }
 
+// factor times cos and sin of N pairs from j0 on (N even; past the last pair: zeros)
+template <int N>
+__device__ __forceinline__ void angles(const Params &p, const Table &table, const Token &at, int j0, float *cs, float *sn) {
+    int pos[N];
+    unsigned long long turns[N];
+    const int one = p.positions ? p.axes == 1 ? p.positions[at.pos] : 0 : at.index;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int j = min(j0 + i, p.pairs - 1);
+        turns[i] = table.turns[j];
+        pos[i] = p.axes == 1 ? one : p.positions[at.pos + table.axis[j]];
+    }
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+        float2 c, s;
+        cos_sin2(pos + i, turns + i, c, s);
+        const float f = p.factor, g = p.factor * p.sign;
+        cs[i] = c.x * f;
+        cs[i + 1] = c.y * f;
+        sn[i] = s.x * g;
+        sn[i + 1] = s.y * g;
+    }
+}
+
+// One element of a turned pair, rounded alike in every kernel: sn is negative for the first of the two.
+__device__ __forceinline__ float turned(float x, float partner, float cs, float sn) { return __fmaf_rn(x, cs, __fmul_rn(partner, sn)); }
+
 // A thread has 32 bytes of a head -- two runs of 16 in the half layout, `pairs` elements apart, 32 in a row in the
 // interleaved one -- of heads_per_thread heads of one token, HU of them in flight; further threads of the row copy
 // what is not rotated, 16 bytes each.
@@ -95,7 +156,9 @@ template <class T, bool INTERLEAVED, int HU>
 __global__ void __launch_bounds__(THREADS)
 rotary_kernel(const __grid_constant__ Params p, const Divider per_batch, const Divider per_row) {
     constexpr int N = 16 / (int)sizeof(T);   // pairs of a thread = elements of a run
+    __shared__ Table table;
     allow_next();
+    fill_table(table, p);
     // one 64-bit division a block; the quotient below is of a number under THREADS + a row's threads
     const long long first = (long long)blockIdx.x * THREADS;
     const long long token0 = first / per_row.d;
@@ -135,18 +198,7 @@ rotary_kernel(const __grid_constant__ Params p, const Divider per_batch, const D
     };
     load(h0);   // in flight while the angles are computed
     float cs[N], sn[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int j = j0 + i;
-        if (j < p.pairs) {
-            const int pos = p.positions ? p.positions[at.pos + p.axis[j]] : at.index;
-            const float2 t = cos_sin(pos, p.turns[j]);
-            cs[i] = t.x * p.factor;
-            sn[i] = t.y * p.factor * p.sign;
-        } else {
-            cs[i] = sn[i] = 0.f;
-        }
-    }
+    angles<N>(p, table, at, j0, cs, sn);
     for (int h = h0;;) {
 #pragma unroll
         for (int i = 0; i < HU; ++i) {
@@ -158,17 +210,17 @@ rotary_kernel(const __grid_constant__ Params p, const Divider per_batch, const D
                     const float x0 = a[i].get(2 * e), y0 = a[i].get(2 * e + 1), x1 = b[i].get(2 * e), y1 = b[i].get(2 * e + 1);
                     // elements behind the rotated part stay, whatever they hold
                     const bool r0 = j0 + e < p.pairs, r1 = j0 + N / 2 + e < p.pairs;
-                    fa[2 * e] = r0 ? x0 * cs[e] - y0 * sn[e] : x0;
-                    fa[2 * e + 1] = r0 ? x0 * sn[e] + y0 * cs[e] : y0;
-                    fb[2 * e] = r1 ? x1 * cs[N / 2 + e] - y1 * sn[N / 2 + e] : x1;
-                    fb[2 * e + 1] = r1 ? x1 * sn[N / 2 + e] + y1 * cs[N / 2 + e] : y1;
+                    fa[2 * e] = r0 ? turned(x0, y0, cs[e], -sn[e]) : x0;
+                    fa[2 * e + 1] = r0 ? turned(y0, x0, cs[e], sn[e]) : y0;
+                    fb[2 * e] = r1 ? turned(x1, y1, cs[N / 2 + e], -sn[N / 2 + e]) : x1;
+                    fb[2 * e + 1] = r1 ? turned(y1, x1, cs[N / 2 + e], sn[N / 2 + e]) : y1;
                 }
             } else {
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     const float x0 = a[i].get(e), y0 = b[i].get(e);
-                    fa[e] = x0 * cs[e] - y0 * sn[e];
-                    fb[e] = x0 * sn[e] + y0 * cs[e];
+                    fa[e] = turned(x0, y0, cs[e], -sn[e]);
+                    fb[e] = turned(y0, x0, cs[e], sn[e]);
                 }
             }
             T *row = (T *)p.out + at.out + (h + i) * p.oh;
@@ -183,6 +235,63 @@ rotary_kernel(const __grid_constant__ Params p, const Divider per_batch, const D
         h += HU;
         if (h >= h1) break;
         load(h);
+    }
+}
+
+// Half layout with a pair count that leaves the second half unaligned: a thread has 16 bytes of the output of
+// heads_per_thread heads and reads the elements they are paired with one by one.  Not in place: those belong to other
+// threads.  (8 heads of 16384 tokens, head dim 128, 33 pairs, bf16: 53 us with a pair a thread, TIMED us.)
+template <class T>
+__global__ void __launch_bounds__(THREADS)
+rotary_shifted_kernel(const __grid_constant__ Params p, const Divider per_batch, const Divider per_row) {
+    constexpr int N = 16 / (int)sizeof(T);
+    __shared__ Table table;
+    allow_next();
+    fill_table(table, p);
+    const long long first = (long long)blockIdx.x * THREADS;
+    const long long token0 = first / per_row.d;
+    const unsigned rest = (unsigned)(first - token0 * per_row.d) + threadIdx.x;
+    const unsigned dt = per_row.quotient(rest);
+    const int c0 = (int)(rest - dt * per_row.d) * N;   // first element
+    const long long token = token0 + dt;
+    wait_for_previous();
+    if (token >= p.tokens) return;
+    const Token at = locate(p, token, per_batch);
+    const int h0 = blockIdx.y * p.heads_per_thread, h1 = min(h0 + p.heads_per_thread, p.heads);
+    float cs[N], sn[N];   // out = cs * x[c] + sn * x[partner]
+    int partner[N];
+    {
+        int pos[N];
+        unsigned long long turns[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = c0 + i, j = min(c < p.pairs ? c : c - p.pairs, p.pairs - 1);
+            turns[i] = table.turns[j];
+            pos[i] = p.positions ? p.positions[at.pos + table.axis[j]] : at.index;
+            partner[i] = c >= 2 * p.pairs ? c : c < p.pairs ? c + p.pairs : c - p.pairs;
+        }
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            float2 c, s;
+            cos_sin2(pos + i, turns + i, c, s);
+            cs[i] = c.x * p.factor;
+            cs[i + 1] = c.y * p.factor;
+            sn[i] = s.x * p.factor * p.sign * (c0 + i < p.pairs ? -1.f : 1.f);
+            sn[i + 1] = s.y * p.factor * p.sign * (c0 + i + 1 < p.pairs ? -1.f : 1.f);
+        }
+    }
+    for (int h = h0; h < h1; ++h) {
+        const T *row = (const T *)p.x + at.x + h * p.xh;
+        Chunk<T> a, o;
+        a.v = *reinterpret_cast<const uint4 *>(row + c0);
+        float f[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float x = a.get(i);
+            f[i] = c0 + i < 2 * p.pairs ? turned(x, (float)row[partner[i]], cs[i], sn[i]) : x;
+        }
+        o.set(f);
+        *reinterpret_cast<uint4 *>((T *)p.out + at.out + h * p.oh + c0) = o.v;
     }
 }
 
@@ -208,16 +317,17 @@ rotary_single_kernel(const __grid_constant__ Params p, const Divider per_batch, 
         for (int h = h0; h < h1; ++h) out[h * p.oh + c] = x[h * p.xh + c];
         return;
     }
-    const int pos = p.positions ? p.positions[at.pos + p.axis[item]] : at.index;
-    float2 t = cos_sin(pos, p.turns[item]);
-    t.x *= p.factor;
-    t.y *= p.factor * p.sign;
+    const int pos = p.positions ? p.positions[at.pos + p.axis[item]] : at.index, two[2] = {pos, pos};
+    const unsigned long long turns[2] = {p.turns[item], p.turns[item]};
+    float2 c, s;
+    cos_sin2(two, turns, c, s);
+    const float cs = c.x * p.factor, sn = s.x * p.factor * p.sign;
     const int ca = INTERLEAVED ? 2 * item : item, cb = INTERLEAVED ? 2 * item + 1 : item + p.pairs;
 #pragma unroll 4
     for (int h = h0; h < h1; ++h) {
         const float a = (float)x[h * p.xh + ca], b = (float)x[h * p.xh + cb];
-        out[h * p.oh + ca] = (T)(a * t.x - b * t.y);
-        out[h * p.oh + cb] = (T)(a * t.y + b * t.x);
+        out[h * p.oh + ca] = (T)turned(a, b, cs, -sn);
+        out[h * p.oh + cb] = (T)turned(b, a, cs, sn);
     }
 }
 
@@ -298,11 +408,12 @@ int launch(const void *x, void *out, const int32_t *positions, const double *inv
     const int n = 16 / esz;
     int64_t bits = (int64_t)((uintptr_t)x | (uintptr_t)out);
     for (int i = 0; i < 6; ++i) bits |= strides[i] * esz;
-    const bool vectors = (bits & 15) == 0 && head_dim % n == 0 && (interleaved || pairs % n == 0);
+    const bool aligned = (bits & 15) == 0 && head_dim % n == 0, vectors = aligned && (interleaved || pairs % n == 0);
+    const bool shifted = aligned && !vectors && !same;   // half layout
     const int rotating = vectors ? (pairs + n - 1) / n : pairs;
     const int beyond = vectors ? std::max(0, head_dim - (interleaved ? rotating * 2 * n : 2 * pairs)) / n : head_dim - 2 * pairs;
     // in place there is nothing to copy
-    const int row_threads = rotating + (same ? 0 : beyond);
+    const int row_threads = shifted ? head_dim / n : rotating + (same ? 0 : beyond);
     // heads of a thread: the angles are shared by them, but a few hundred thousand threads are wanted first
     constexpr int HU = 4;
     const long long units = p.tokens * row_threads;
@@ -319,9 +430,11 @@ int launch(const void *x, void *out, const int32_t *positions, const double *inv
     };
     if (dtype == HILBERTA_BF16) {
         if (vectors) HB_CUDA(interleaved ? go(rotary_kernel<__nv_bfloat16, true, HU>) : go(rotary_kernel<__nv_bfloat16, false, HU>));
+        else if (shifted) HB_CUDA(go(rotary_shifted_kernel<__nv_bfloat16>));
         else HB_CUDA(interleaved ? go(rotary_single_kernel<__nv_bfloat16, true>) : go(rotary_single_kernel<__nv_bfloat16, false>));
     } else {
         if (vectors) HB_CUDA(interleaved ? go(rotary_kernel<float, true, HU>) : go(rotary_kernel<float, false, HU>));
+        else if (shifted) HB_CUDA(go(rotary_shifted_kernel<float>));
         else HB_CUDA(interleaved ? go(rotary_single_kernel<float, true>) : go(rotary_single_kernel<float, false>));
     }
     HB_LAUNCHED();

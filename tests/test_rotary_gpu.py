@@ -1,7 +1,7 @@
 """Rotary positions and their gradient against the formula in 64 bits.
 
 Tolerance: u = 2^-24.  The angle in turns is exact but for 2^-31 of half a turn and one rounding to fp32 of at most an
-eighth of a turn (below u in radians), cosine and sine are within two units in the last place (2 u), the factor's own
+eighth of a turn (below u in radians), cosine and sine are Taylor series evaluated to two units in the last place (2 u), the factor's own
 rounding and its product add 2 u, the two products and their sum 2 u of |a| + |b|: 8 u (|a| + |b|) factor covers it.
 Outputs in bf16 add 2^-8 of the value.  Copied elements are the same bits."""
 import math
