@@ -25,7 +25,10 @@ using namespace ptx;
 namespace {
 
 constexpr int BM = 128, BN = 128, QT = 2;
-constexpr int NSTAGE = 5;                // K / V ring slots (K0 V0 K1 V1 ...)
+// K / V ring slots (K0 V0 K1 V1 ...); beside them 32 KB in which finished rows wait for their bulk stores, 4 KB a warp
+constexpr int NSTAGE = 5;
+__host__ __device__ constexpr int ring_slots(int hd) { return hd == 128 ? 4 : NSTAGE; }
+constexpr int STAGE_BYTES = 8 * 4096;
 constexpr int UNITS = 2;                 // units found ahead
 constexpr int SLAB_BYTES = BN * 128;     // 64 columns of 128 rows
 constexpr int THREADS = 384;
@@ -33,7 +36,7 @@ constexpr uint32_t TMEM_COLS = 512;
 constexpr float RESCALE_THRESHOLD = 8.0f;   // log2: the reference maximum moves only when a score exceeds it by 2^8
 constexpr int SPLIT_AT = 2;              // P goes to the MMA issuer as the keys of 32-key chunks 0 .. 2, then the rest
 __host__ __device__ constexpr int tile_bytes(int hd) { return BN * hd * 2; }
-__host__ __device__ constexpr int smem_bytes(int hd) { return (QT + NSTAGE) * tile_bytes(hd) + 1024; }
+__host__ __device__ constexpr int smem_bytes(int hd) { return (QT + ring_slots(hd)) * tile_bytes(hd) + STAGE_BYTES + 1024; }
 
 enum Bar {
     Q_FULL = 0, Q_EMPTY, DRAIN,
@@ -55,7 +58,6 @@ struct Params {
     __nv_bfloat16 *out;
     float *lse;
     float scale_log2;
-    int align32;
 };
 
 // What every role derives from a unit.
@@ -110,23 +112,23 @@ __device__ __forceinline__ void issue_pv(uint32_t tmem_o, uint32_t tmem_p, uint3
 template <int HD>
 __global__ void __launch_bounds__(THREADS, 1)
 packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-              const __grid_constant__ CUtensorMap tmV, const __grid_constant__ Params prm) {
+              const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmO, const __grid_constant__ Params prm) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t bars[NUM_BARS];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     __shared__ packed::Unit units[UNITS];
     constexpr int TILE_BYTES = tile_bytes(HD);
-    constexpr int NSLAB = HD / 64;
+    constexpr int NSLAB = HD / 64, NS = ring_slots(HD);
 
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    const uint32_t sQ = smem_u32(smem), sKV = sQ + QT * TILE_BYTES;
+    const uint32_t sQ = smem_u32(smem), sKV = sQ + QT * TILE_BYTES, sStage = sKV + NS * TILE_BYTES;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t bar0 = smem_u32(&bars[0]);
     int *const status = g_status;
     auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
-    auto slot_of = [](uint32_t e) { return e % NSTAGE; };
-    auto phase_of = [](uint32_t e) { return (e / NSTAGE) & 1; };
+    auto slot_of = [](uint32_t e) { return e % NS; };
+    auto phase_of = [](uint32_t e) { return (e / NS) & 1; };
 
     if (tid == 0) {
         abort_flag = 0;
@@ -445,22 +447,48 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             const bool in = tok < w.len;
             const int head = w.head0 + (r & ((1 << prm.g_shift) - 1));
             const float inv = 1.f / (l + l_fix);
-            __nv_bfloat16 *orow = prm.out + (long long)(w.row0 + tok) * prm.stride_t + (long long)head * prm.stride_h;
             if (prm.lse && in)
                 prm.lse[(long long)head * prm.seq.total + w.row0 + tok] = 0.6931471805599453f * (m_ref + log2f(l));
+            // Rows through shared memory and one bulk tensor store per 64 columns and warp where the warp's 32 rows (32 / g
+            // tokens of g heads: a box) all belong to the sequence; else per lane, rows behind it dropped.
+            const int warp_tok = w.tok0 + ((t * BM + (warp & 3) * 32) >> prm.g_shift);
+            if (warp_tok + (32 >> prm.g_shift) <= w.len) {
+                const uint32_t stage = sStage + warp * 4096;
 #pragma unroll
-            for (int c = 0; c < HD / 32; ++c) {
-                uint32_t o[32];
-                tmem_ld32(tO + c * 32, o);
-                tmem_wait_ld();
-                if (in) {
-                    uint32_t v[16];
+                for (int rd = 0; rd < HD / 64; ++rd) {
+                    // the bulk store that last used the space has read it
+                    if (lane == 0) bulk_wait_group_read0();
+                    __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = pack_bf16(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
-                    if (prm.align32) {
-                        st_global_v8(orow + c * 32, v);
-                        st_global_v8(orow + c * 32 + 16, v + 8);
-                    } else {
+                    for (int c2 = 0; c2 < 2; ++c2) {
+                        uint32_t o[32];
+                        tmem_ld32(tO + rd * 64 + c2 * 32, o);
+                        tmem_wait_ld();
+                        uint32_t v[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[i] = pack_bf16(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
+                        // row `lane` of a 128-byte-swizzled box: 16-byte chunk k sits at k ^ (row & 7)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) st_shared_v4(stage + lane * 128 + (((c2 * 4 + k) ^ (lane & 7)) << 4), v + 4 * k);
+                    }
+                    fence_proxy_async_smem();   // generic-proxy writes -> the bulk copy's reads
+                    __syncwarp();
+                    if (lane == 0) {
+                        tma_store_4d(&tmO, stage, 64 * rd, w.head0, w.row0 + warp_tok, 0);
+                        bulk_commit_group();
+                    }
+                }
+            } else {
+                __nv_bfloat16 *orow = prm.out + (long long)(w.row0 + tok) * prm.stride_t + (long long)head * prm.stride_h;
+#pragma unroll
+                for (int c = 0; c < HD / 32; ++c) {
+                    uint32_t o[32];
+                    tmem_ld32(tO + c * 32, o);
+                    tmem_wait_ld();
+                    if (in) {
+                        uint32_t v[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[i] = pack_bf16(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
 #pragma unroll
                         for (int i = 0; i < 16; i += 4)
                             *reinterpret_cast<uint4 *>(orow + c * 32 + 2 * i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
@@ -471,13 +499,12 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             release();
         }
     }
+    // the epilogue's bulk stores are complete before the CTA gives up its shared memory
+    if (warp < 8 && lane == 0) bulk_wait_group0();
     tc_fence_before();
     __syncthreads();
     __syncwarp();
-    if (warp == 8) {
-        __syncwarp();
-        tmem_dealloc(tmem, TMEM_COLS);
-    }
+    if (warp == 8) tmem_dealloc(tmem, TMEM_COLS);
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
@@ -631,15 +658,15 @@ extern "C" int hilberta_packed_forward(const void *q, const void *k, const void 
     p.lse = lse;
     const float s = scale > 0.f ? scale : 1.f / sqrtf((float)head_dim);
     p.scale_log2 = s * 1.4426950408889634f;
-    p.align32 = ((uintptr_t)out & 31) == 0 && ((strides[6] | strides[7]) & 15) == 0;
-    CUtensorMap mq, mk, mv;
+    CUtensorMap mq, mk, mv, mo;
     if ((rc = packed::make_map(&mq, q, total, heads, head_dim, strides[0], strides[1], g, per_tile)) != HILBERTA_OK) return rc;
     if ((rc = packed::make_map(&mk, k, total, kv_heads, head_dim, strides[2], strides[3], 1, BN)) != HILBERTA_OK) return rc;
     if ((rc = packed::make_map(&mv, v, total, kv_heads, head_dim, strides[4], strides[5], 1, BN)) != HILBERTA_OK) return rc;
+    if ((rc = packed::make_map(&mo, out, total, heads, head_dim, strides[6], strides[7], g, 32 / g)) != HILBERTA_OK) return rc;
     const unsigned ctas = (unsigned)std::min((long long)sms, units(p.tiles));
     const bool overlap = (size_t)total * heads * head_dim * 2 <= kOverlapBytes / 4;
     HB_CUDA(launch_overlapping(head_dim == 128 ? packed_kernel<128> : packed_kernel<64>, ctas, THREADS, (size_t)smem_bytes(head_dim), 1,
-                               (cudaStream_t)stream, overlap, mq, mk, mv, p));
+                               (cudaStream_t)stream, overlap, mq, mk, mv, mo, p));
     HB_LAUNCHED();
     return HILBERTA_OK;
 }
