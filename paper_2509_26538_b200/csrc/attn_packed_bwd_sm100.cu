@@ -45,7 +45,8 @@ enum Bar {
     T1_FULL = P_READY + 2, T1_EMPTY = T1_FULL + NT1,
     T2_FULL = T1_EMPTY + NT1, T2_EMPTY = T2_FULL + NT2,
     SHORT = T2_EMPTY + NT2,       // the element-wise threads among themselves (256 arrivals)
-    U_FULL = SHORT + 1, U_EMPTY = U_FULL + UNITS,   // U_EMPTY: two producers, issuer, 8 element-wise and 4 epilogue warps
+    NEXT, WANT,                   // see the forward kernel
+    U_FULL, U_EMPTY = U_FULL + UNITS,   // U_EMPTY: two producers, issuer, 8 element-wise and 4 epilogue warps
     NUM_BARS = U_EMPTY + UNITS
 };
 constexpr int UNIT_READERS = 15;
@@ -54,7 +55,8 @@ constexpr int OFF_R1 = 0, OFF_R2 = TILE_BYTES, OFF_T1 = 2 * TILE_BYTES, OFF_T2 =
 constexpr int OFF_STAT = OFF_T2 + NT2 * TILE_BYTES;
 constexpr int OFF_BARS = OFF_STAT + NT2 * STAT_BYTES;
 constexpr int OFF_UNITS = OFF_BARS + NUM_BARS * 8;
-constexpr int OFF_MISC = OFF_UNITS + UNITS * 16;
+constexpr int OFF_NEXT = (OFF_UNITS + UNITS * 20 + 15) / 16 * 16;
+constexpr int OFF_MISC = OFF_NEXT + 16;
 constexpr int SMEM_USED = OFF_MISC + 16;
 constexpr int SMEM_BYTES = 232448;   // the 227 KB a CTA may have; SMEM_USED and the gap to a 1024-byte boundary must fit
 static_assert(SMEM_USED <= SMEM_BYTES, "shared memory of one CTA");
@@ -64,7 +66,7 @@ __device__ int g_status[64];
 struct Params {
     packed::Sequences queries, keys;   // blocks of a DQ unit (128 / g tokens) and of a DKV unit (128 tokens)
     int kv_heads, odd, group, g_shift, heads;   // group = odd << g_shift
-    int dkv_ctas;
+    unsigned dkv_units;   // CTAs of the launch that stand for units of the DKV mode
     const float *lse2, *delta;   // [total, heads]
     __nv_bfloat16 *dq, *dk, *dv;
     long long dq_t, dq_h, dk_t, dk_h, dv_t, dv_h;
@@ -134,9 +136,13 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const void *src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 
-template <int MODE, int HD>
-__device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorMap &tmR2, const CUtensorMap &tmT1,
-                                        const CUtensorMap &tmT2, const Params &prm, int cta, int ctas) {
+// Every role goes through the CTA's units, DKV units and then DQ units, with code of its own for each mode; barriers and
+// rings do not care which it is.
+template <int HD>
+__global__ void __launch_bounds__(THREADS, 1)
+packed_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                  const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmdO,
+                  const __grid_constant__ Params prm) {
     extern __shared__ uint8_t smem_raw[];
     constexpr uint32_t REG_A = 0, REG_B = 128, OUT_A = 256, OUT_B = 384;   // TMEM columns
     constexpr int NSLAB = HD / 64;
@@ -158,7 +164,6 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
     int *const status = g_status;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int g_shift = prm.g_shift;
-    const int reps = MODE == MODE_DKV ? prm.odd : 1;   // head parts that are streamed one after the other
     auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
 
     if (tid == 0) {
@@ -167,8 +172,8 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
             uint32_t count = 1;
             if (i == EPI_DONE) count = 128;
             if (i == A_DONE || i == P_READY || i == P_READY + 1 || i == SHORT) count = 256;
-            // DKV: ring 2 also carries the row statistics, copied by the 32 lanes of its producer warp
-            if (MODE == MODE_DKV && i >= T2_FULL && i < T2_FULL + NT2) count = 33;
+            // ring 2 also carries the row statistics (DKV), copied by the 32 lanes of its producer warp
+            if (i >= T2_FULL && i < T2_FULL + NT2) count = 33;
             if (i >= U_EMPTY) count = UNIT_READERS;
             mbar_init(bar(i), count);
         }
@@ -196,6 +201,8 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
         return u.len >= 0;
     };
 
+    using Dq = std::integral_constant<int, MODE_DQ>;
+    using Dkv = std::integral_constant<int, MODE_DKV>;
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     }
@@ -203,32 +210,27 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
         // ------------------------------------------------ producers of the streamed blocks
         // warp 8 feeds ring 1 (K_j in DQ mode, Q_i in DKV mode), warp 10 ring 2 (V_j / dO_i and, in DKV mode, the
         // statistics of the streamed query rows)
-        const bool second = warp == 10;
-        const bool with_stats = MODE == MODE_DKV && second;   // whole warp takes part
-        const bool leader = with_stats ? lane == 0 : elect_one();
-        if (leader || with_stats) {
-            const CUtensorMap *tm = second ? &tmT2 : &tmT1;
-            if (leader) prefetch_tmap(tm);
+        const bool second = warp == 10;   // the whole warp takes part
+        const bool leader = second ? lane == 0 : elect_one();
+        if (leader || second) {
             const int nslot = second ? NT2 : NT1;
             const int FULL = second ? T2_FULL : T1_FULL, EMPTY = second ? T2_EMPTY : T1_EMPTY;
             const uint32_t ring = second ? sT2 : sT1;
-            const int tps = MODE == MODE_DKV ? BK >> g_shift : BK;   // tokens of a streamed block
             uint32_t g = 0;
             bool ok = true;
-            packed::Unit u;
-            for (;;) {
-                ok = next_unit(u, false, 0x400 + (second ? 1 : 0));
-                if (with_stats) ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                if (leader) mbar_arrive(bar(U_EMPTY + (uc - 1) % UNITS));
+            auto stream = [&](auto mode, const packed::Unit &u) {
+                constexpr int MODE = decltype(mode)::value;
+                const CUtensorMap *tm = MODE == MODE_DKV ? (second ? &tmdO : &tmQ) : (second ? &tmV : &tmK);
+                const int tps = MODE == MODE_DKV ? BK >> g_shift : BK;   // tokens of a streamed block
                 const Work w = work_of<MODE>(prm, u);
-                for (int rep = 0; ok && rep < reps; ++rep) {
+                // head parts that are streamed one after the other
+                for (int rep = 0; ok && rep < (MODE == MODE_DKV ? prm.odd : 1); ++rep) {
                     const int head = MODE == MODE_DKV ? w.head0 + (rep << g_shift) : w.kv_head;
                     for (int j = 0; j < w.count; ++j, ++g) {
                         const int tok = (w.first + j) * tps;
                         const uint32_t s = g % nslot, ph = (g / nslot) & 1;
                         if (leader) ok = wait_or_abort(bar(EMPTY + s), ph ^ 1, abort_flag, status, 0x402 + (second ? 1 : 0));
-                        if (with_stats) ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+                        if (second) ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
                         if (!ok) break;
                         if (leader) {
                             const uint32_t dst = ring + s * TILE_BYTES;
@@ -237,12 +239,12 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
                             for (int sl = 0; sl < NSLAB; ++sl)
                                 tma_load_4d(dst + sl * SLAB_BYTES, tm, bar(FULL + s), 64 * sl, head, w.row0 + tok, 0);
                         }
-                        if (with_stats) {
-                            // the block's rows that belong to the sequence (the others are masked by position later);
-                            // the arrival fires when the copies land
+                        if (second) {
+                            // DKV: statistics of the block's rows that belong to the sequence (the others are masked by position
+                            // later); the arrival fires when the copies land
                             const uint32_t sdst = sbase + OFF_STAT + s * STAT_BYTES;
 #pragma unroll
-                            for (int i = 0; i < BK / 32; ++i) {
+                            for (int i = 0; MODE == MODE_DKV && i < BK / 32; ++i) {
                                 const int c = lane + 32 * i, t = tok + (c >> g_shift);
                                 if (t < w.len) {
                                     const long long at = (long long)(w.row0 + t) * prm.heads + head + (c & ((1 << g_shift) - 1));
@@ -254,9 +256,19 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
                         }
                     }
                 }
+            };
+            packed::Unit u;
+            for (;;) {
+                ok = next_unit(u, false, 0x400 + (second ? 1 : 0));
+                if (second) ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
+                if (leader) mbar_arrive(bar(U_EMPTY + (uc - 1) % UNITS));
+                if (u.mode == MODE_DKV) stream(Dkv{}, u);
+                else stream(Dq{}, u);
+                if (!ok) break;
+                if (leader && !second) mbar_arrive(bar(WANT));
             }
-            if (with_stats) asm volatile("cp.async.wait_all;" ::: "memory");
+            if (second) asm volatile("cp.async.wait_all;" ::: "memory");
             if (*abort_flag && leader) {
                 // let every copy already issued land before the CTA retires
                 const long long t0 = clock64();
@@ -266,38 +278,71 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
         }
     } else if (warp == 11) {
         // ------------------------------------------------ finds the units and loads their resident tiles
-        prefetch_tmap(&tmR1);
-        prefetch_tmap(&tmR2);
-        packed::Runs runs;
-        const packed::Sequences seq = MODE == MODE_DQ ? prm.queries : prm.keys;
-        const int parts = MODE == MODE_DQ ? prm.kv_heads * prm.odd : prm.kv_heads;
-        for (int round = 0;; ++round) {
-            packed::Unit u;
-            const bool found = packed::find_unit(seq, runs, parts, cta, ctas, round, u);
-            if (!found) u.len = -1;
-            bool ok = true;
+        if (lane == 0) {
+            prefetch_tmap(&tmQ);
+            prefetch_tmap(&tmK);
+            prefetch_tmap(&tmV);
+            prefetch_tmap(&tmdO);
+        }
+        packed::Runs key_runs, query_runs;
+        const packed::Span key_span = packed::span_of(prm.keys, lane), query_span = packed::span_of(prm.queries, lane);
+        const uint32_t next = sbase + OFF_NEXT;
+        unsigned n = blockIdx.x;
+        uint32_t asked = 0;
+        bool more = true, ok = true;
+        auto find = [&](packed::Unit &u) {
+            u.mode = n < prm.dkv_units ? MODE_DKV : MODE_DQ;
+            return n < prm.dkv_units ? packed::find_unit(prm.keys, key_span, key_runs, prm.kv_heads, n, u)
+                                     : packed::find_unit(prm.queries, query_span, query_runs, prm.kv_heads * prm.odd, n - prm.dkv_units, u);
+        };
+        auto ask_next = [&] {
             if (lane == 0) {
-                const uint32_t s = round % UNITS;
-                ok = wait_or_abort(bar(U_EMPTY + s), ((round / UNITS) & 1) ^ 1, abort_flag, status, 0x406);
+                fence_proxy_async_smem();   // the last answer has been read
+                packed::ask_next_cta(next, bar(NEXT));
+                ok = wait_or_abort(bar(NEXT), asked & 1, abort_flag, status, 0x407);
+                if (ok) more = packed::next_cta(next, n);
+            }
+            ++asked;
+            n = __shfl_sync(0xffffffffu, n, 0);
+            more = __shfl_sync(0xffffffffu, (int)more, 0) != 0;
+            ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+        };
+        for (uint32_t i = 0; ok; ++i) {
+            packed::Unit u;
+            // the launch has a CTA for every unit there may be; some are not there
+            bool found = more && find(u);
+            while (ok && more && !found) {
+                ask_next();
+                found = ok && more && find(u);
+            }
+            if (!ok) break;
+            if (!found) u.len = -1;
+            if (lane == 0) {
+                const uint32_t s = i % UNITS;
+                ok = wait_or_abort(bar(U_EMPTY + s), ((i / UNITS) & 1) ^ 1, abort_flag, status, 0x406);
                 if (ok) {
                     units[s] = u;
                     mbar_arrive(bar(U_FULL + s));
                     // free once the last R T^T MMA of the previous unit has retired
-                    if (found && round > 0) ok = wait_or_abort(bar(RES_EMPTY), (round - 1) & 1, abort_flag, status, 0x401);
+                    if (found && i > 0) ok = wait_or_abort(bar(RES_EMPTY), (i - 1) & 1, abort_flag, status, 0x401);
                     if (found && ok) {
-                        const Work w = work_of<MODE>(prm, u);
-                        const int head = MODE == MODE_DQ ? w.head0 : w.kv_head;
+                        const bool dkv = u.mode == MODE_DKV;
+                        const Work w = dkv ? work_of<MODE_DKV>(prm, u) : work_of<MODE_DQ>(prm, u);
+                        const int head = dkv ? w.kv_head : w.head0;
                         mbar_expect_tx(bar(RES_FULL), 2 * TILE_TX);
 #pragma unroll
                         for (int sl = 0; sl < NSLAB; ++sl) {
-                            tma_load_4d(sR1 + sl * SLAB_BYTES, &tmR1, bar(RES_FULL), 64 * sl, head, w.row0 + w.tok0, 0);
-                            tma_load_4d(sR2 + sl * SLAB_BYTES, &tmR2, bar(RES_FULL), 64 * sl, head, w.row0 + w.tok0, 0);
+                            tma_load_4d(sR1 + sl * SLAB_BYTES, dkv ? &tmK : &tmQ, bar(RES_FULL), 64 * sl, head, w.row0 + w.tok0, 0);
+                            tma_load_4d(sR2 + sl * SLAB_BYTES, dkv ? &tmV : &tmdO, bar(RES_FULL), 64 * sl, head, w.row0 + w.tok0, 0);
                         }
+                        // not before the producer is through with this unit: one that another CTA could start sooner is left to it
+                        ok = wait_or_abort(bar(WANT), i & 1, abort_flag, status, 0x408);
                     }
                 }
             }
             ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
             if (!found || !ok) break;
+            ask_next();
         }
         if (*abort_flag && lane == 0) {
             const long long t0 = clock64();
@@ -316,39 +361,44 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
             __syncwarp();
             if (!ok) break;
             if (lane == 0) mbar_arrive(bar(U_EMPTY + (uc - 1) % UNITS));
-            const Work w = work_of<MODE>(prm, u);
             ok = wait_or_abort(bar(OUT_FULL), n & 1, abort_flag, status, 0x607);
             if (!ok) break;
             tc_fence_after();
-            const int tok = w.tok0 + (MODE == MODE_DQ ? r >> g_shift : r);
-            const int head = MODE == MODE_DQ ? w.head0 + (r & ((1 << g_shift) - 1)) : w.kv_head;
-            const long long row = w.row0 + tok;
-            __nv_bfloat16 *const out_a = MODE == MODE_DQ ? prm.dq + row * prm.dq_t + head * prm.dq_h : prm.dk + row * prm.dk_t + head * prm.dk_h;
-            __nv_bfloat16 *const out_b = prm.dv + row * prm.dv_t + head * prm.dv_h;
-            constexpr int CPO = HD / 32;                              // 32-column chunks per output
-            constexpr int NCH = (MODE == MODE_DKV) ? 2 * CPO : CPO;   // DKV: dK then dV
+            auto store = [&](auto mode) {
+                constexpr int MODE = decltype(mode)::value;
+                const Work w = work_of<MODE>(prm, u);
+                const int tok = w.tok0 + (MODE == MODE_DQ ? r >> g_shift : r);
+                const int head = MODE == MODE_DQ ? w.head0 + (r & ((1 << g_shift) - 1)) : w.kv_head;
+                const long long row = w.row0 + tok;
+                __nv_bfloat16 *const out_a = MODE == MODE_DQ ? prm.dq + row * prm.dq_t + head * prm.dq_h : prm.dk + row * prm.dk_t + head * prm.dk_h;
+                __nv_bfloat16 *const out_b = prm.dv + row * prm.dv_t + head * prm.dv_h;
+                constexpr int CPO = HD / 32;                              // 32-column chunks per output
+                constexpr int NCH = (MODE == MODE_DKV) ? 2 * CPO : CPO;   // DKV: dK then dV
 #pragma unroll
-            for (int c = 0; c < NCH; ++c) {
-                uint32_t o[32];
-                tmem_ld32(tmem + lane_addr + (c >= CPO ? OUT_B + (c - CPO) * 32 : OUT_A + c * 32), o);
-                tmem_wait_ld();
-                if (tok < w.len) {
-                    __nv_bfloat16 *orow = (c >= CPO ? out_b : out_a) + (c % CPO) * 32;
-                    const float mul = c >= CPO ? 1.f : prm.scale;
-                    uint32_t v[16];
+                for (int c = 0; c < NCH; ++c) {
+                    uint32_t o[32];
+                    tmem_ld32(tmem + lane_addr + (c >= CPO ? OUT_B + (c - CPO) * 32 : OUT_A + c * 32), o);
+                    tmem_wait_ld();
+                    if (tok < w.len) {
+                        __nv_bfloat16 *orow = (c >= CPO ? out_b : out_a) + (c % CPO) * 32;
+                        const float mul = c >= CPO ? 1.f : prm.scale;
+                        uint32_t v[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        v[i] = pack_bf16(__uint_as_float(o[2 * i]) * mul, __uint_as_float(o[2 * i + 1]) * mul);
-                    if (prm.align32) {
-                        st_global_v8(orow, v);
-                        st_global_v8(orow + 16, v + 8);
-                    } else {
+                        for (int i = 0; i < 16; ++i)
+                            v[i] = pack_bf16(__uint_as_float(o[2 * i]) * mul, __uint_as_float(o[2 * i + 1]) * mul);
+                        if (prm.align32) {
+                            st_global_v8(orow, v);
+                            st_global_v8(orow + 16, v + 8);
+                        } else {
 #pragma unroll
-                        for (int i = 0; i < 16; i += 4)
-                            *reinterpret_cast<uint4 *>(orow + 2 * i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                            for (int i = 0; i < 16; i += 4)
+                                *reinterpret_cast<uint4 *>(orow + 2 * i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                        }
                     }
                 }
-            }
+            };
+            if (u.mode == MODE_DKV) store(Dkv{});
+            else store(Dq{});
             tc_fence_before();
             mbar_arrive(bar(EPI_DONE));
         }
@@ -359,20 +409,19 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
             bool ok = true;
             auto t1 = [&](uint32_t e) { return sT1 + (e % NT1) * TILE_BYTES; };
             auto t2 = [&](uint32_t e) { return sT2 + (e % NT2) * TILE_BYTES; };
-            packed::Unit u;
-            for (; ok && next_unit(u, true, 0x500); ++n_unit) {
-                const Work w = work_of<MODE>(prm, u);
-                const int n = w.count * reps;
+            auto multiply = [&](auto mode, const packed::Unit &u) {
+                constexpr int MODE = decltype(mode)::value;
+                const int n = work_of<MODE>(prm, u).count * (MODE == MODE_DKV ? prm.odd : 1);
                 ok = wait_or_abort(bar(RES_FULL), n_unit & 1, abort_flag, status, 0x501);
-                if (!ok) break;
+                if (!ok) return;
                 // scores and dP of the first block
                 ok = wait_or_abort(bar(T1_FULL + g % NT1), (g / NT1) & 1, abort_flag, status, 0x502);
-                if (!ok) break;
+                if (!ok) return;
                 tc_fence_after();
                 issue_rt<HD>(tmem + REG_A, sR1, t1(g));
                 mma_commit(bar(S_FULL));
                 ok = wait_or_abort(bar(T2_FULL + g % NT2), (g / NT2) & 1, abort_flag, status, 0x503);
-                if (!ok) break;
+                if (!ok) return;
                 tc_fence_after();
                 issue_rt<HD>(tmem + REG_B, sR2, t2(g));
                 mma_commit(bar(DP_FULL));
@@ -418,9 +467,14 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
                         if (s + 2 == n) mma_commit(bar(RES_EMPTY));   // last read of the resident tiles
                     }
                 }
-                if (!ok) break;
+                if (!ok) return;
                 mma_commit(bar(OUT_FULL));
                 g += n;
+            };
+            packed::Unit u;
+            for (; ok && next_unit(u, true, 0x500); ++n_unit) {
+                if (u.mode == MODE_DKV) multiply(Dkv{}, u);
+                else multiply(Dq{}, u);
             }
             // every MMA issued above has retired before TMEM is released
             mma_commit(bar(DRAIN));
@@ -446,190 +500,209 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
             __syncwarp();
             if (!any) break;
             if (lane == 0) mbar_arrive(bar(U_EMPTY + (uc - 1) % UNITS));
-            const Work w = work_of<MODE>(prm, u);
-            // DQ: this thread's query row; rows behind the sequence get lse = +inf, which turns their weights into zeros
-            float row_l2 = __int_as_float(0x7f800000), row_dl = 0.f;
-            const int tok = w.tok0 + (MODE == MODE_DQ ? r >> g_shift : r);   // the query's (DQ) or the key's (DKV) token
-            if (MODE == MODE_DQ && tok < w.len) {
-                const long long at = (long long)(w.row0 + tok) * prm.heads + w.head0 + (r & ((1 << g_shift) - 1));
-                row_l2 = __ldg(prm.lse2 + at);
-                row_dl = __ldg(prm.delta + at);
-            }
-            for (int rep = 0; ok && rep < reps; ++rep) {
-                for (int j = 0; j < w.count; ++j, ++g) {
-                    // Pairs that exist: streamed columns lo <= c < hi of this warpgroup's 64; dS is zero below lo_ds
-                    // (and above hi_ds) too, since a query with one key has no gradient through its weight of one.
-                    int lo = 0, hi = 64, lo_ds = 0, hi_ds = 64, beyond;   // beyond: the block's rows of the sequence
-                    bool masked;
-                    if (MODE == MODE_DQ) {
-                        beyond = w.len - j * BK;
-                        const int end = (prm.queries.causal ? min(tok + 1, w.len) : w.len);
-                        masked = (j + 1) * BK > (prm.queries.causal ? min(w.tok0 + 1, w.len) : w.len);
-                        hi = end - j * BK - wg * 64;
-                        hi_ds = end == 1 ? 0 : hi;
-                    } else {
-                        const int t0 = (w.first + j) << (7 - g_shift);
-                        beyond = (w.len - t0) << g_shift;
-                        masked = beyond < BK || w.len == 1;
-                        hi = beyond - wg * 64;
-                        if (prm.keys.causal) {
-                            masked |= t0 < w.tok0 + BM;
-                            lo = (tok - t0) * (1 << g_shift) - wg * 64;
-                            lo_ds = max(lo, (1 - t0) * (1 << g_shift) - wg * 64);
-                        } else if (w.len == 1) {
-                            lo_ds = 64;
-                        }
-                    }
-                    float *const slot = stats + (MODE == MODE_DKV ? (g % NT2) * (2 * BK) : 0);   // lse2, then delta
-                    const float4 *const st_l = reinterpret_cast<const float4 *>(slot + wg * 64), *const st_d = st_l + BK / 4;
-                    if (MODE == MODE_DKV) {
-                        // the statistics arrive with ring 2
-                        ok = wait_or_abort(bar(T2_FULL + g % NT2), (g / NT2) & 1, abort_flag, status, 0x602);
-                        if (!ok) break;
-                    }
-                    // ---- phase 1: weights from the scores
-                    ok = wait_or_abort(bar(S_FULL), g & 1, abort_flag, status, 0x603 + wg);
-                    if (!ok) break;
-                    tc_fence_after();
-                    uint32_t a[64];
-                    tmem_ld32(tA, *reinterpret_cast<uint32_t(*)[32]>(&a[0]));
-                    tmem_ld32(tA + 32, *reinterpret_cast<uint32_t(*)[32]>(&a[32]));
-                    tmem_wait_ld();
-                    tc_fence_before();
-                    mbar_arrive(bar(A_DONE));   // region A may take the next block's scores
-                    auto phase1 = [&](auto MASKED) {
-#pragma unroll
-                        for (int c4 = 0; c4 < 16; ++c4) {
-                            float4 l4 = make_float4(row_l2, row_l2, row_l2, row_l2);
-                            if (MODE == MODE_DKV) l4 = st_l[c4];
-                            const float2 x0 = __ffma2_rn(make_float2(__uint_as_float(a[4 * c4]), __uint_as_float(a[4 * c4 + 1])),
-                                                         make_float2(scale_log2, scale_log2), make_float2(-l4.x, -l4.y));
-                            const float2 x1 = __ffma2_rn(make_float2(__uint_as_float(a[4 * c4 + 2]), __uint_as_float(a[4 * c4 + 3])),
-                                                         make_float2(scale_log2, scale_log2), make_float2(-l4.z, -l4.w));
-                            float p[4] = {ex2(x0.x), ex2(x0.y), ex2(x1.x), ex2(x1.y)};
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                if (decltype(MASKED)::value && (4 * c4 + i < lo || 4 * c4 + i >= hi)) p[i] = 0.f;
-                                a[4 * c4 + i] = __float_as_uint(p[i]);
+            auto weigh = [&](auto mode) {
+                constexpr int MODE = decltype(mode)::value;
+                const Work w = work_of<MODE>(prm, u);
+                // DQ: this thread's query row; rows behind the sequence get lse = +inf, which turns their weights into zeros
+                float row_l2 = __int_as_float(0x7f800000), row_dl = 0.f;
+                const int tok = w.tok0 + (MODE == MODE_DQ ? r >> g_shift : r);   // the query's (DQ) or the key's (DKV) token
+                if (MODE == MODE_DQ && tok < w.len) {
+                    const long long at = (long long)(w.row0 + tok) * prm.heads + w.head0 + (r & ((1 << g_shift) - 1));
+                    row_l2 = __ldg(prm.lse2 + at);
+                    row_dl = __ldg(prm.delta + at);
+                }
+                for (int rep = 0; ok && rep < (MODE == MODE_DKV ? prm.odd : 1); ++rep) {
+                    for (int j = 0; j < w.count; ++j, ++g) {
+                        // Pairs that exist: streamed columns lo <= c < hi of this warpgroup's 64; dS is zero below lo_ds
+                        // (and above hi_ds) too, since a query with one key has no gradient through its weight of one.
+                        int lo = 0, hi = 64, lo_ds = 0, hi_ds = 64, beyond;   // beyond: the block's rows of the sequence
+                        bool masked;
+                        if (MODE == MODE_DQ) {
+                            beyond = w.len - j * BK;
+                            const int end = (prm.queries.causal ? min(tok + 1, w.len) : w.len);
+                            masked = (j + 1) * BK > (prm.queries.causal ? min(w.tok0 + 1, w.len) : w.len);
+                            hi = end - j * BK - wg * 64;
+                            hi_ds = end == 1 ? 0 : hi;
+                        } else {
+                            const int t0 = (w.first + j) << (7 - g_shift);
+                            beyond = (w.len - t0) << g_shift;
+                            masked = beyond < BK || w.len == 1;
+                            hi = beyond - wg * 64;
+                            if (prm.keys.causal) {
+                                masked |= t0 < w.tok0 + BM;
+                                lo = (tok - t0) * (1 << g_shift) - wg * 64;
+                                lo_ds = max(lo, (1 - t0) * (1 << g_shift) - wg * 64);
+                            } else if (w.len == 1) {
+                                lo_ds = 64;
                             }
                         }
-                    };
-                    if (masked) phase1(std::true_type{});
-                    else phase1(std::false_type{});
-                    // ---- phase 2: dS = P * (dP - delta), written over dP together with P
-                    ok = wait_or_abort(bar(DP_FULL), g & 1, abort_flag, status, 0x605 + wg);
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (beyond < BK) {
-                        // Streamed rows behind the sequence belong to others: weights and dS are zero there, and so
-                        // are the rows themselves from here on, whatever they hold.  Both products that read them
-                        // for A and B are done; those that multiply them by zeros wait for P_READY.
-                        if ((MODE == MODE_DKV || wg == 0) && r >= beyond) {
-                            const uint32_t base = (wg == 0 ? sT1 + (g % NT1) * TILE_BYTES : sT2 + (g % NT2) * TILE_BYTES) + r * 128;
-                            const uint32_t zero[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-                            for (int c = 0; c < NSLAB * 8; ++c) st_shared_v4(base + (c >> 3) * SLAB_BYTES + (c & 7) * 16, zero);
+                        float *const slot = stats + (g % NT2) * (2 * BK);   // DKV: lse2, then delta
+                        const float4 *const st_l = reinterpret_cast<const float4 *>(slot + wg * 64), *const st_d = st_l + BK / 4;
+                        if (MODE == MODE_DKV) {
+                            // the statistics arrive with ring 2
+                            ok = wait_or_abort(bar(T2_FULL + g % NT2), (g / NT2) & 1, abort_flag, status, 0x602);
+                            if (!ok) break;
                         }
-                        fence_proxy_async_smem();
-                    }
-                    const bool exact = w.len <= BK;   // the row's or column's delta from this block alone
-                    if (exact) {
-                        float sum[2] = {0.f, 0.f};   // DQ: of this row; DKV: of columns lane and 32 + lane over this warp's keys
+                        // ---- phase 1: weights from the scores
+                        ok = wait_or_abort(bar(S_FULL), g & 1, abort_flag, status, 0x603 + wg);
+                        if (!ok) break;
+                        tc_fence_after();
+                        uint32_t a[64];
+                        tmem_ld32(tA, *reinterpret_cast<uint32_t(*)[32]>(&a[0]));
+                        tmem_ld32(tA + 32, *reinterpret_cast<uint32_t(*)[32]>(&a[32]));
+                        tmem_wait_ld();
+                        tc_fence_before();
+                        mbar_arrive(bar(A_DONE));   // region A may take the next block's scores
+                        auto phase1 = [&](auto MASKED) {
 #pragma unroll
-                        for (int h2 = 0; h2 < 2; ++h2) {
-                            uint32_t d[32];
-                            float x[32];
-                            tmem_ld32(tB + h2 * 32, d);
-                            tmem_wait_ld();
+                            for (int c4 = 0; c4 < 16; ++c4) {
+                                float4 l4 = make_float4(row_l2, row_l2, row_l2, row_l2);
+                                if (MODE == MODE_DKV) l4 = st_l[c4];
+                                const float2 x0 = __ffma2_rn(make_float2(__uint_as_float(a[4 * c4]), __uint_as_float(a[4 * c4 + 1])),
+                                                             make_float2(scale_log2, scale_log2), make_float2(-l4.x, -l4.y));
+                                const float2 x1 = __ffma2_rn(make_float2(__uint_as_float(a[4 * c4 + 2]), __uint_as_float(a[4 * c4 + 3])),
+                                                             make_float2(scale_log2, scale_log2), make_float2(-l4.z, -l4.w));
+                                float p[4] = {ex2(x0.x), ex2(x0.y), ex2(x1.x), ex2(x1.y)};
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                // a weight of zero, whatever the other factor; keys behind the sequence count for nothing
-                                const float p = __uint_as_float(a[h2 * 32 + i]);
-                                x[i] = p == 0.f || (MODE == MODE_DKV && tok >= w.len) ? 0.f : p * __uint_as_float(d[i]);
+                                for (int i = 0; i < 4; ++i) {
+                                    if (decltype(MASKED)::value && (4 * c4 + i < lo || 4 * c4 + i >= hi)) p[i] = 0.f;
+                                    a[4 * c4 + i] = __float_as_uint(p[i]);
+                                }
+                            }
+                        };
+                        if (masked) phase1(std::true_type{});
+                        else phase1(std::false_type{});
+                        // ---- phase 2: dS = P * (dP - delta), written over dP together with P
+                        ok = wait_or_abort(bar(DP_FULL), g & 1, abort_flag, status, 0x605 + wg);
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (beyond < BK) {
+                            // Streamed rows behind the sequence belong to others: weights and dS are zero there, and so
+                            // are the rows themselves from here on, whatever they hold.  Both products that read them
+                            // for A and B are done; those that multiply them by zeros wait for P_READY.
+                            if ((MODE == MODE_DKV || wg == 0) && r >= beyond) {
+                                const uint32_t base = (wg == 0 ? sT1 + (g % NT1) * TILE_BYTES : sT2 + (g % NT2) * TILE_BYTES) + r * 128;
+                                const uint32_t zero[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+                                for (int c = 0; c < NSLAB * 8; ++c) st_shared_v4(base + (c >> 3) * SLAB_BYTES + (c & 7) * 16, zero);
+                            }
+                            fence_proxy_async_smem();
+                        }
+                        const bool exact = w.len <= BK;   // the row's or column's delta from this block alone
+                        if (exact) {
+                            float sum[2] = {0.f, 0.f};   // DQ: of this row; DKV: of columns lane and 32 + lane over this warp's keys
+#pragma unroll
+                            for (int h2 = 0; h2 < 2; ++h2) {
+                                uint32_t d[32];
+                                float x[32];
+                                tmem_ld32(tB + h2 * 32, d);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) {
+                                    // a weight of zero, whatever the other factor; keys behind the sequence count for nothing
+                                    const float p = __uint_as_float(a[h2 * 32 + i]);
+                                    x[i] = p == 0.f || (MODE == MODE_DKV && tok >= w.len) ? 0.f : p * __uint_as_float(d[i]);
+                                }
+                                if (MODE == MODE_DQ) {
+#pragma unroll
+                                    for (int i = 0; i < 32; ++i) sum[0] += x[i];
+                                } else {
+                                    // lane c is left with the sum of column c: each step hands half of the columns over
+#pragma unroll
+                                    for (int o = 16; o > 0; o >>= 1) {
+                                        const bool up = (lane & o) != 0;
+#pragma unroll
+                                        for (int i = 0; i < o; ++i) {
+                                            const float keep = up ? x[i + o] : x[i], give = up ? x[i] : x[i + o];
+                                            x[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+                                        }
+                                    }
+                                    sum[h2] = x[0];
+                                }
                             }
                             if (MODE == MODE_DQ) {
-#pragma unroll
-                                for (int i = 0; i < 32; ++i) sum[0] += x[i];
+                                // the other 64 columns' sum through tensor memory, in the place of this thread's first dP for a while
+                                const uint32_t dp0 = tmem_ld1(tB);
+                                tmem_wait_ld();
+                                tmem_st1(tB, __float_as_uint(sum[0]));
+                                tmem_wait_st();
+                                tc_fence_before();
+                                ok = meet();
+                                if (!ok) break;
+                                tc_fence_after();
+                                const uint32_t other = tmem_ld1(tmem + lane_addr + REG_B + (1 - wg) * 64);
+                                tmem_wait_ld();
+                                tc_fence_before();
+                                ok = meet();
+                                if (!ok) break;
+                                tc_fence_after();
+                                tmem_st1(tB, dp0);
+                                tmem_wait_st();
+                                row_dl = wg ? __uint_as_float(other) + sum[0] : sum[0] + __uint_as_float(other);
                             } else {
-                                // lane c is left with the sum of column c: each step hands half of the columns over
-#pragma unroll
-                                for (int o = 16; o > 0; o >>= 1) {
-                                    const bool up = (lane & o) != 0;
-#pragma unroll
-                                    for (int i = 0; i < o; ++i) {
-                                        const float keep = up ? x[i + o] : x[i], give = up ? x[i] : x[i + o];
-                                        x[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
-                                    }
-                                }
-                                sum[h2] = x[0];
+                                // four warps' sums become two in the place of lse2 and delta, which nobody needs any more
+                                float *const to = slot + (warp & 1) * BK + wg * 64 + lane;
+                                ok = meet();
+                                if (!ok) break;
+                                if ((warp & 2) == 0) to[0] = sum[0], to[32] = sum[1];
+                                ok = meet();
+                                if (!ok) break;
+                                if ((warp & 2) != 0) to[0] += sum[0], to[32] += sum[1];
+                                ok = meet();
+                                if (!ok) break;
                             }
                         }
-                        if (MODE == MODE_DQ) {
-                            slot[wg * BK + r] = sum[0];
-                            ok = meet();
-                            if (!ok) break;
-                            row_dl = slot[r] + slot[BK + r];
-                        } else {
-                            // four warps' sums become two in the place of lse2 and delta, which nobody needs any more
-                            float *const to = slot + (warp & 1) * BK + wg * 64 + lane;
-                            ok = meet();
-                            if (!ok) break;
-                            if ((warp & 2) == 0) to[0] = sum[0], to[32] = sum[1];
-                            ok = meet();
-                            if (!ok) break;
-                            if ((warp & 2) != 0) to[0] += sum[0], to[32] += sum[1];
-                            ok = meet();
-                            if (!ok) break;
-                        }
+                        auto phase2 = [&](auto MASKED) {
+#pragma unroll
+                            for (int h2 = 0; h2 < 2; ++h2) {
+                                uint32_t d[32];
+                                tmem_ld32(tB + h2 * 32, d);
+                                tmem_wait_ld();
+                                uint32_t pk[16], dk[16];
+#pragma unroll
+                                for (int i4 = 0; i4 < 8; ++i4) {
+                                    const int c0 = h2 * 32 + 4 * i4;
+                                    float4 d4 = make_float4(row_dl, row_dl, row_dl, row_dl);
+                                    if (MODE == MODE_DKV) {
+                                        d4 = st_d[c0 >> 2];
+                                        if (decltype(MASKED)::value && exact) {
+                                            const float4 e4 = st_l[c0 >> 2];
+                                            d4.x += e4.x, d4.y += e4.y, d4.z += e4.z, d4.w += e4.w;
+                                        }
+                                    }
+                                    const float2 pa = make_float2(__uint_as_float(a[c0]), __uint_as_float(a[c0 + 1]));
+                                    const float2 pb = make_float2(__uint_as_float(a[c0 + 2]), __uint_as_float(a[c0 + 3]));
+                                    const float2 sa = __fmul2_rn(__fadd2_rn(make_float2(__uint_as_float(d[4 * i4]), __uint_as_float(d[4 * i4 + 1])),
+                                                                            make_float2(-d4.x, -d4.y)), pa);
+                                    const float2 sb = __fmul2_rn(__fadd2_rn(make_float2(__uint_as_float(d[4 * i4 + 2]), __uint_as_float(d[4 * i4 + 3])),
+                                                                            make_float2(-d4.z, -d4.w)), pb);
+                                    float s[4] = {sa.x, sa.y, sb.x, sb.y};
+                                    if (decltype(MASKED)::value) {
+                                        // P is zero there already; dP - delta may be anything
+#pragma unroll
+                                        for (int i = 0; i < 4; ++i)
+                                            if (c0 + i < max(lo, lo_ds) || c0 + i >= min(hi, hi_ds)) s[i] = 0.f;
+                                    }
+                                    pk[2 * i4] = pack_bf16(pa.x, pa.y);
+                                    pk[2 * i4 + 1] = pack_bf16(pb.x, pb.y);
+                                    dk[2 * i4] = pack_bf16(s[0], s[1]);
+                                    dk[2 * i4 + 1] = pack_bf16(s[2], s[3]);
+                                }
+                                // the 32 columns just read take P (16 columns of bf16 pairs) and dS (16)
+                                if (MODE == MODE_DKV) tmem_st16(tB + h2 * 32, pk);
+                                tmem_st16(tB + h2 * 32 + 16, dk);
+                                tmem_wait_st();
+                                tc_fence_before();
+                                mbar_arrive(bar(P_READY + h2));
+                            }
+                        };
+                        if (masked || exact) phase2(std::true_type{});
+                        else phase2(std::false_type{});
                     }
-                    auto phase2 = [&](auto MASKED) {
-#pragma unroll
-                        for (int h2 = 0; h2 < 2; ++h2) {
-                            uint32_t d[32];
-                            tmem_ld32(tB + h2 * 32, d);
-                            tmem_wait_ld();
-                            uint32_t pk[16], dk[16];
-#pragma unroll
-                            for (int i4 = 0; i4 < 8; ++i4) {
-                                const int c0 = h2 * 32 + 4 * i4;
-                                float4 d4 = make_float4(row_dl, row_dl, row_dl, row_dl);
-                                if (MODE == MODE_DKV) {
-                                    d4 = st_d[c0 >> 2];
-                                    if (decltype(MASKED)::value && exact) {
-                                        const float4 e4 = st_l[c0 >> 2];
-                                        d4.x += e4.x, d4.y += e4.y, d4.z += e4.z, d4.w += e4.w;
-                                    }
-                                }
-                                const float2 pa = make_float2(__uint_as_float(a[c0]), __uint_as_float(a[c0 + 1]));
-                                const float2 pb = make_float2(__uint_as_float(a[c0 + 2]), __uint_as_float(a[c0 + 3]));
-                                const float2 sa = __fmul2_rn(__fadd2_rn(make_float2(__uint_as_float(d[4 * i4]), __uint_as_float(d[4 * i4 + 1])),
-                                                                        make_float2(-d4.x, -d4.y)), pa);
-                                const float2 sb = __fmul2_rn(__fadd2_rn(make_float2(__uint_as_float(d[4 * i4 + 2]), __uint_as_float(d[4 * i4 + 3])),
-                                                                        make_float2(-d4.z, -d4.w)), pb);
-                                float s[4] = {sa.x, sa.y, sb.x, sb.y};
-                                if (decltype(MASKED)::value) {
-                                    // P is zero there already; dP - delta may be anything
-#pragma unroll
-                                    for (int i = 0; i < 4; ++i)
-                                        if (c0 + i < max(lo, lo_ds) || c0 + i >= min(hi, hi_ds)) s[i] = 0.f;
-                                }
-                                pk[2 * i4] = pack_bf16(pa.x, pa.y);
-                                pk[2 * i4 + 1] = pack_bf16(pb.x, pb.y);
-                                dk[2 * i4] = pack_bf16(s[0], s[1]);
-                                dk[2 * i4 + 1] = pack_bf16(s[2], s[3]);
-                            }
-                            // the 32 columns just read take P (16 columns of bf16 pairs) and dS (16)
-                            if (MODE == MODE_DKV) tmem_st16(tB + h2 * 32, pk);
-                            tmem_st16(tB + h2 * 32 + 16, dk);
-                            tmem_wait_st();
-                            tc_fence_before();
-                            mbar_arrive(bar(P_READY + h2));
-                        }
-                    };
-                    if (masked || exact) phase2(std::true_type{});
-                    else phase2(std::false_type{});
                 }
-            }
+            };
+            if (u.mode == MODE_DKV) weigh(Dkv{});
+            else weigh(Dq{});
         }
     }
 
@@ -637,17 +710,6 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap &tmR1, const CUtensorM
     __syncthreads();
     __syncwarp();
     if (warp == 8) tmem_dealloc(tmem, TMEM_COLS);
-}
-
-// The first CTAs work in DKV mode, whose blocks take longer, the others in DQ mode, which take the SMs as they fall idle.
-template <int HD>
-__global__ void __launch_bounds__(THREADS, 1)
-packed_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                  const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmdO,
-                  const __grid_constant__ Params prm) {
-    const int cta = (int)blockIdx.x, dkv = prm.dkv_ctas;
-    if (cta < dkv) bwd_cta<MODE_DKV, HD>(tmK, tmV, tmQ, tmdO, prm, cta, dkv);
-    else bwd_cta<MODE_DQ, HD>(tmQ, tmdO, tmK, tmV, prm, cta - dkv, (int)gridDim.x - dkv);
 }
 
 // lse2[t, h] = lse[h, t] * log2 e, delta[t, h] = sum_d dO[t, h, d] * O[t, h, d]: HD / 8 lanes per row (16 bytes each),
@@ -784,11 +846,9 @@ extern "C" int hilberta_packed_backward(const void *dout, const void *q, const v
                                (const __nv_bfloat16 *)dout, (const __nv_bfloat16 *)out, lse, lse2, delta, total, heads, (long long)strides[0],
                                (long long)strides[1], (long long)strides[8], (long long)strides[9]));
     HB_LAUNCHED();
-    auto units = [&](int per, int parts) {
-        return std::min((long long)sms, ((long long)total / per + std::min(n_seq, total)) * parts);
-    };
-    p.dkv_ctas = (int)units(BM, kv_heads);
-    const unsigned ctas = (unsigned)(p.dkv_ctas + units(per_tile, kv_heads * p.odd));
+    auto units = [&](int per, int parts) { return (unsigned)(((long long)total / per + std::min(n_seq, total)) * parts); };   // at most
+    p.dkv_units = units(BM, kv_heads);
+    const unsigned ctas = p.dkv_units + units(per_tile, kv_heads * p.odd);
     HB_CUDA(launch_overlapping(head_dim == 128 ? packed_bwd_kernel<128> : packed_bwd_kernel<64>, ctas, THREADS, (size_t)SMEM_BYTES, 1, st,
                                true, mq, mk, mv, mdo, p));
     HB_LAUNCHED();

@@ -8,7 +8,7 @@
 // Causal: a tile ends with the block of its last token; the keys behind a row's token in that block, and those behind
 // the end of the sequence, are masked by column.
 //
-// Roles of a CTA (one per SM, persistent):
+// Roles of a CTA (one per SM; it goes on with the units of CTAs that have not started):
 //   warps 0-3  softmax and epilogue of query tile 0, thread r owns row r (TMEM lane r); warps 4-7 tile 1
 //   warp 8     TMA producer   warp 9  MMA issuer   warp 10  finds the units, two ahead   warp 11 idle
 // The two tiles take turns: while one tile's softmax runs, the tensor core works on the other's P V and next Q K^T.
@@ -44,7 +44,9 @@ enum Bar {
     P_READY = S_FULL + QT,        // [2 t + part], 128 arrivals
     PV_DONE = P_READY + 2 * QT,
     KV_FULL = PV_DONE + QT, KV_EMPTY = KV_FULL + NSTAGE,
-    U_FULL = KV_EMPTY + NSTAGE, U_EMPTY = U_FULL + UNITS,   // U_EMPTY: producer, issuer, eight softmax warps
+    NEXT = KV_EMPTY + NSTAGE,                               // the number of the next CTA has arrived
+    WANT = NEXT + 1,                                        // the producer has asked for all of a unit's blocks
+    U_FULL = WANT + 1, U_EMPTY = U_FULL + UNITS,            // U_EMPTY: producer, issuer, eight softmax warps
     NUM_BARS = U_EMPTY + UNITS
 };
 
@@ -118,6 +120,7 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     __shared__ packed::Unit units[UNITS];
+    __shared__ __align__(16) uint4 next[1];
     constexpr int TILE_BYTES = tile_bytes(HD);
     constexpr int NSLAB = HD / 64, NS = ring_slots(HD);
 
@@ -151,6 +154,21 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     allow_next();
     wait_for_previous();
 
+    // the number of the next CTA that has not started, for a whole warp
+    auto ask_next = [&](unsigned &n, bool &more, uint32_t &asked) {
+        bool ok = true;
+        if (lane == 0) {
+            fence_proxy_async_smem();   // the last answer has been read
+            packed::ask_next_cta(smem_u32(next), bar(NEXT));
+            ok = wait_or_abort(bar(NEXT), asked & 1, &abort_flag, status, 0x109);
+            if (ok) more = packed::next_cta(smem_u32(next), n);
+        }
+        ++asked;
+        n = __shfl_sync(0xffffffffu, n, 0);
+        more = __shfl_sync(0xffffffffu, (int)more, 0) != 0;
+        return __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+    };
+
     // the next unit, for a role of one thread
     uint32_t uc = 0;
     auto next_unit = [&](packed::Unit &u, int code) {
@@ -168,12 +186,20 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     if (warp == 10) {
         // ------------------------------------------------------------ finds the units
         packed::Runs runs;
-        for (int round = 0;; ++round) {
+        const packed::Span mine = packed::span_of(prm.seq, lane);
+        unsigned n = blockIdx.x;
+        bool more = true, ok = true;
+        for (uint32_t i = 0, asked = 0; ok; ++i) {
             packed::Unit u;
-            const bool found = packed::find_unit(prm.seq, runs, prm.parts, blockIdx.x, gridDim.x, round, u);
+            // the launch has a CTA for every unit there may be; some are not there
+            bool found = more && packed::find_unit(prm.seq, mine, runs, prm.parts, n, u);
+            while (ok && more && !found) {
+                ok = ask_next(n, more, asked);
+                found = ok && more && packed::find_unit(prm.seq, mine, runs, prm.parts, n, u);
+            }
+            if (!ok) break;
             if (!found) u.len = -1;
-            const uint32_t s = round % UNITS, ph = (round / UNITS) & 1;
-            bool ok = true;
+            const uint32_t s = i % UNITS, ph = (i / UNITS) & 1;
             if (lane == 0) {
                 ok = wait_or_abort(bar(U_EMPTY + s), ph ^ 1, &abort_flag, status, 0x108);
                 if (ok) {
@@ -183,6 +209,9 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             }
             ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
             if (!found || !ok) break;
+            // not before the producer is through with this unit: a unit that another CTA could start sooner is left to it
+            if (lane == 0) ok = wait_or_abort(bar(WANT), i & 1, &abort_flag, status, 0x10a);
+            ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0 && ask_next(n, more, asked);
         }
     } else if (warp == 8) {
         // ------------------------------------------------------------ producer
@@ -218,6 +247,7 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 const int n = max(w.n[0], w.n[1]);
                 for (int j = 0; ok && j < n; ++j)
                     ok = emit(&tmK, w.row0 + j * BN, w.kv_head) && emit(&tmV, w.row0 + j * BN, w.kv_head);
+                mbar_arrive(bar(WANT));
             }
             if (abort_flag) {
                 // let every copy already issued land before the CTA retires
@@ -566,6 +596,7 @@ int check(const void *const *tensors, int n, const int64_t *strides, const int32
     if (dtype == HILBERTA_FP32 || dtype == HILBERTA_FP8_E4M3) return HILBERTA_ERR_UNSUPPORTED;
     if (dtype != HILBERTA_BF16 || head_dim < 1) return HILBERTA_ERR_INVALID;
     if ((head_dim != 64 && head_dim != 128) || n_seq > MAX_SEQ || total > MAX_TOTAL || heads > 65536) return HILBERTA_ERR_UNSUPPORTED;
+    if ((long long)total * heads > (1ll << 31) - (1ll << 24)) return HILBERTA_ERR_UNSUPPORTED;   // units are counted in 31 bits
     if ((uintptr_t)cu & 3) return HILBERTA_ERR_INVALID;
     for (int i = 0; i < n; ++i) {
         const int64_t st = strides[2 * i], sh = strides[2 * i + 1];
@@ -663,7 +694,7 @@ extern "C" int hilberta_packed_forward(const void *q, const void *k, const void 
     if ((rc = packed::make_map(&mk, k, total, kv_heads, head_dim, strides[2], strides[3], 1, BN)) != HILBERTA_OK) return rc;
     if ((rc = packed::make_map(&mv, v, total, kv_heads, head_dim, strides[4], strides[5], 1, BN)) != HILBERTA_OK) return rc;
     if ((rc = packed::make_map(&mo, out, total, heads, head_dim, strides[6], strides[7], g, 32 / g)) != HILBERTA_OK) return rc;
-    const unsigned ctas = (unsigned)std::min((long long)sms, units(p.tiles));
+    const unsigned ctas = (unsigned)units(p.tiles);
     const bool overlap = (size_t)total * heads * head_dim * 2 <= kOverlapBytes / 4;
     HB_CUDA(launch_overlapping(head_dim == 128 ? packed_kernel<128> : packed_kernel<64>, ctas, THREADS, (size_t)smem_bytes(head_dim), 1,
                                (cudaStream_t)stream, overlap, mq, mk, mv, mo, p));
