@@ -66,8 +66,8 @@ __device__ __forceinline__ bool find_block(const Sequences &s, const Span &mine,
     for (;;) {
         const unsigned in_run = (unsigned)(s.causal ? st.top - st.low + 1 : st.low) * (unsigned)st.count;
         if (k < st.before + in_run) break;
+        if (st.low == 0) return false;   // the last run stays: more of the missing blocks may be asked for
         st.before += in_run;
-        if (st.low == 0) return false;
         st.top = st.low - 1;
         int count = 0, low = 0;
         for (int i = 0; i < s.n; i += 32) {
