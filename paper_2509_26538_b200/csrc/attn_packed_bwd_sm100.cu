@@ -716,22 +716,32 @@ packed_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 // four rows in flight per lane group.  Rows outside the sequences are read like the others and used by nobody.
 template <int HD>
 __global__ void __launch_bounds__(256)
-packed_delta_kernel(const __nv_bfloat16 *dout, const __nv_bfloat16 *out, const float *lse, float *lse2, float *delta, int total, int heads,
+packed_delta_kernel(const __nv_bfloat16 *dout, const __nv_bfloat16 *out, const float *lse, float *lse2, float *delta, int total, Divider heads,
                     long long do_t, long long do_h, long long o_t, long long o_h) {
     constexpr int LPR = HD / 8;
-    const int sub = threadIdx.x % LPR;
-    const long long n_rows = (long long)total * heads, row0 = ((long long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR) * 4;
+    const unsigned sub = threadIdx.x % LPR, n_rows = (unsigned)total * heads.d;   // below 2^31, see the host
+    const unsigned row0 = (blockIdx.x * (256 / LPR) + threadIdx.x / LPR) * 4;
+    unsigned t[4], h[4];
+    t[0] = heads.quotient(row0);
+    h[0] = row0 - t[0] * heads.d;
+#pragma unroll
+    for (int i = 1; i < 4; ++i) {
+        const bool wrap = h[i - 1] + 1 == heads.d;
+        h[i] = wrap ? 0 : h[i - 1] + 1;
+        t[i] = t[i - 1] + (wrap ? 1 : 0);
+    }
     uint4 a[4], c[4];
+    float l[4];
     allow_next();
     wait_for_previous();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const long long row = row0 + i;
         a[i] = c[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (row < n_rows) {
-            const long long t = row / heads, h = row % heads;
-            a[i] = *reinterpret_cast<const uint4 *>(dout + t * do_t + h * do_h + sub * 8);
-            c[i] = *reinterpret_cast<const uint4 *>(out + t * o_t + h * o_h + sub * 8);
+        l[i] = 0.f;
+        if (row0 + i < n_rows) {
+            a[i] = *reinterpret_cast<const uint4 *>(dout + t[i] * do_t + h[i] * do_h + sub * 8);
+            c[i] = *reinterpret_cast<const uint4 *>(out + t[i] * o_t + h[i] * o_h + sub * 8);
+            if (sub == 0) l[i] = lse[(long long)h[i] * total + t[i]];
         }
     }
 #pragma unroll
@@ -746,10 +756,9 @@ packed_delta_kernel(const __nv_bfloat16 *dout, const __nv_bfloat16 *out, const f
         }
 #pragma unroll
         for (int o = LPR / 2; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
-        const long long row = row0 + i;
-        if (row < n_rows && sub == 0) {
-            lse2[row] = lse[(row % heads) * total + row / heads] * 1.4426950408889634f;
-            delta[row] = acc;
+        if (row0 + i < n_rows && sub == 0) {
+            lse2[row0 + i] = l[i] * 1.4426950408889634f;
+            delta[row0 + i] = acc;
         }
     }
 }
@@ -843,7 +852,7 @@ extern "C" int hilberta_packed_backward(const void *dout, const void *q, const v
     const long long blocks = ((long long)total * heads + rows_per_block - 1) / rows_per_block;
     if (blocks > 0x7fffffffll) return HILBERTA_ERR_UNSUPPORTED;
     HB_CUDA(launch_overlapping(head_dim == 128 ? packed_delta_kernel<128> : packed_delta_kernel<64>, (unsigned)blocks, 256, 0, 1, st, overlap,
-                               (const __nv_bfloat16 *)dout, (const __nv_bfloat16 *)out, lse, lse2, delta, total, heads, (long long)strides[0],
+                               (const __nv_bfloat16 *)dout, (const __nv_bfloat16 *)out, lse, lse2, delta, total, Divider(heads), (long long)strides[0],
                                (long long)strides[1], (long long)strides[8], (long long)strides[9]));
     HB_LAUNCHED();
     auto units = [&](int per, int parts) { return (unsigned)(((long long)total / per + std::min(n_seq, total)) * parts); };   // at most
