@@ -133,32 +133,39 @@ layer_norm_kernel(const ForwardParams prm) {
         return v;
     };
     const T *x = (const T *)prm.x + row * prm.stride_x;
+    // Vectors of one element go through the arithmetic two by two.
+    constexpr int STEP = VEC > 1 ? 1 : 2, P = VEC > 1 ? VEC / 2 : 1;   // vectors and pairs at a time
+    static_assert(NV % STEP == 0, "single elements come in pairs");
+    auto col = [&](int i) { return (i * LANES + lane) * VEC; };
     Vec<T, VEC> v[NV];
-    float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (i * LANES + lane) * VEC;
-        if (in && c < cols) v[i].load(x + c);
+        if (in && col(i) < cols) v[i].load(x + col(i));
         else v[i].zero();
     }
+    auto pair = [&](int i, int e) { return VEC > 1 ? v[i].pair(e) : make_float2(v[i].get(0), v[(i + 1) % NV].get(0)); };
+    float2 acc[2] = {both(0.f), both(0.f)};   // two chains
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; i += STEP)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sum += v[i].get(e);
-    const float mean = row_sum(sum, 0) / (float)cols;
-    float sq = 0.f;
+        for (int e = 0; e < P; ++e) acc[(i + e) & 1] = __fadd2_rn(acc[(i + e) & 1], pair(i, e));
+    acc[0] = __fadd2_rn(acc[0], acc[1]);
+    const float mean = row_sum(acc[0].x + acc[0].y, 0) / (float)cols;
+    const float2 shift = both(-mean);
+    acc[0] = acc[1] = both(0.f);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (i * LANES + lane) * VEC;
-        if (c < cols) {
+    for (int i = 0; i < NV; i += STEP) {
+        if (col(i) < cols) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const float d = v[i].get(e) - mean;
-                sq = fmaf(d, d, sq);
+            for (int e = 0; e < P; ++e) {
+                float2 d = __fadd2_rn(pair(i, e), shift);
+                if (VEC == 1 && col(i + 1) >= cols) d.y = 0.f;
+                acc[(i + e) & 1] = __ffma2_rn(d, d, acc[(i + e) & 1]);
             }
         }
     }
-    const float rstd = 1.f / sqrtf(row_sum(sq, 1) / (float)cols + prm.eps);
+    acc[0] = __fadd2_rn(acc[0], acc[1]);
+    const float rstd = 1.f / sqrtf(row_sum(acc[0].x + acc[0].y, 1) / (float)cols + prm.eps);
     if (!in) return;
     if (lane == 0) {
         if (prm.mean) prm.mean[row] = mean;
@@ -168,28 +175,43 @@ layer_norm_kernel(const ForwardParams prm) {
     const W *w = prm.weight ? (const W *)prm.weight + group * prm.stride_w : nullptr;
     const W *b = prm.bias ? (const W *)prm.bias + group * prm.stride_w : nullptr;
     T *y = (T *)prm.y + row * prm.stride_y;
+    const float2 scale = both(rstd), offset = both(prm.offset);
+    auto weights = [&](float2 *to, const W *from, int i) {
+        Vec<W, VEC> t;
+        t.load(from + col(i));
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (i * LANES + lane) * VEC;
-        if (c >= cols) continue;
-        float f[VEC];
+        for (int e = 0; e < P; ++e) to[e] = t.pair(e);
+        if (VEC == 1 && col(i + 1) < cols) {
+            t.load(from + col(i + 1));
+            to[0].y = t.get(0);
+        }
+    };
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) f[e] = (v[i].get(e) - mean) * rstd;
+    for (int i = 0; i < NV; i += STEP) {
+        if (col(i) >= cols) continue;
+        float2 f[P], t[P];
+#pragma unroll
+        for (int e = 0; e < P; ++e) f[e] = __fmul2_rn(__fadd2_rn(pair(i, e), shift), scale);
         if (w) {
-            Vec<W, VEC> t;
-            t.load(w + c);
+            weights(t, w, i);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) f[e] *= t.get(e) + prm.offset;
+            for (int e = 0; e < P; ++e) f[e] = __fmul2_rn(f[e], __fadd2_rn(t[e], offset));
         }
         if (b) {
-            Vec<W, VEC> t;
-            t.load(b + c);
+            weights(t, b, i);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) f[e] += t.get(e);
+            for (int e = 0; e < P; ++e) f[e] = __fadd2_rn(f[e], t[e]);
         }
+        float out[2 * P];
+#pragma unroll
+        for (int e = 0; e < P; ++e) out[2 * e] = f[e].x, out[2 * e + 1] = f[e].y;
         Vec<T, VEC> o;
-        o.set(f);
-        o.store(y + c);
+        o.set(out);
+        o.store(y + col(i));
+        if (VEC == 1 && col(i + 1) < cols) {
+            o.set(out + 1);
+            o.store(y + col(i + 1));
+        }
     }
 }
 
