@@ -19,7 +19,7 @@ namespace hilberta {
 namespace {
 
 constexpr int MAX_PAIRS = 128;   // head dim <= 256
-constexpr int THREADS = 256;
+constexpr int THREADS = 128;
 
 struct Params {
     const void *x;
@@ -226,10 +226,10 @@ rotary_kernel(const __grid_constant__ Params p, const Divider per_batch, const D
             T *row = (T *)p.out + at.out + (h + i) * p.oh;
             Chunk<T> o;
             o.set(fa);
-            *reinterpret_cast<uint4 *>(row + ca) = o.v;
+            __stcs(reinterpret_cast<uint4 *>(row + ca), o.v);
             if (!INTERLEAVED || cb < p.dim) {
                 o.set(fb);
-                *reinterpret_cast<uint4 *>(row + cb) = o.v;
+                __stcs(reinterpret_cast<uint4 *>(row + cb), o.v);
             }
         }
         h += HU;
@@ -414,8 +414,9 @@ int launch(const void *x, void *out, const int32_t *positions, const double *inv
     const int beyond = vectors ? std::max(0, head_dim - (interleaved ? rotating * 2 * n : 2 * pairs)) / n : head_dim - 2 * pairs;
     // in place there is nothing to copy
     const int row_threads = shifted ? head_dim / n : rotating + (same ? 0 : beyond);
-    // heads of a thread: the angles are shared by them, but a few hundred thousand threads are wanted first
-    constexpr int HU = 4;
+    // Heads of a thread: the angles are shared by them, but a few hundred thousand threads are wanted first.  Four of them in
+    // flight, or two where a thread has no more (registers: 100000 tokens of one head of 64, us, 4 / 2: 10.6 / 8.5; 24 heads of
+    // 16384 tokens 33.8 / 36.0).
     const long long units = p.tokens * row_threads;
     int hpt = 1;
     while (hpt < 8 && hpt < heads && units * ((heads + hpt * 2 - 1) / (hpt * 2)) >= (long long)sms * 1024) hpt *= 2;
@@ -429,11 +430,13 @@ int launch(const void *x, void *out, const int32_t *positions, const double *inv
         return launch_overlapping(kernel, grid, THREADS, 0, 1, stream, overlap, p, Divider(S), Divider(row_threads));
     };
     if (dtype == HILBERTA_BF16) {
-        if (vectors) HB_CUDA(interleaved ? go(rotary_kernel<__nv_bfloat16, true, HU>) : go(rotary_kernel<__nv_bfloat16, false, HU>));
+        if (vectors) HB_CUDA(hpt >= 4 ? (interleaved ? go(rotary_kernel<__nv_bfloat16, true, 4>) : go(rotary_kernel<__nv_bfloat16, false, 4>))
+                                 : (interleaved ? go(rotary_kernel<__nv_bfloat16, true, 2>) : go(rotary_kernel<__nv_bfloat16, false, 2>)));
         else if (shifted) HB_CUDA(go(rotary_shifted_kernel<__nv_bfloat16>));
         else HB_CUDA(interleaved ? go(rotary_single_kernel<__nv_bfloat16, true>) : go(rotary_single_kernel<__nv_bfloat16, false>));
     } else {
-        if (vectors) HB_CUDA(interleaved ? go(rotary_kernel<float, true, HU>) : go(rotary_kernel<float, false, HU>));
+        if (vectors) HB_CUDA(hpt >= 4 ? (interleaved ? go(rotary_kernel<float, true, 4>) : go(rotary_kernel<float, false, 4>))
+                                 : (interleaved ? go(rotary_kernel<float, true, 2>) : go(rotary_kernel<float, false, 2>)));
         else if (shifted) HB_CUDA(go(rotary_shifted_kernel<float>));
         else HB_CUDA(interleaved ? go(rotary_single_kernel<float, true>) : go(rotary_single_kernel<float, false>));
     }
