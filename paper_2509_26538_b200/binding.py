@@ -418,9 +418,9 @@ def _scratch(n, like, stream):
     """n bytes of torch's memory that belong to the stream of the call, so that they are reused in its order."""
     import torch
     if stream is None:
-        return torch.empty(n, dtype=torch.uint8, device=like.device)
+        return like.new_empty(n, dtype=torch.uint8)
     with torch.cuda.stream(stream):
-        return torch.empty(n, dtype=torch.uint8, device=like.device)
+        return like.new_empty(n, dtype=torch.uint8)
 
 
 def _ptr(t):
@@ -448,27 +448,28 @@ def _row_stride(t, name):
 
 def _norm_weights(x, a, b):
     """(rows per group, row stride, dtype code) of weight and bias, or of their gradients: [cols] or [groups, cols]."""
-    w = a if a is not None else b
+    w = b if a is None else a
     if w is None:
         return 0, 0, _dtype_code(x)
-    shape, cols = w.shape, x.shape[-1]
-    if b is not None and b is not w and (b.shape != shape or b.dtype != w.dtype or b.stride() != w.stride()):
+    shape, stride, xshape = w.shape, w.stride(), x.shape
+    cols = xshape[-1]
+    if a is not None and b is not None and (b.shape != shape or b.dtype != w.dtype or b.stride() != stride):
         raise ValueError("weight and bias (and their gradients): one shape, dtype and row stride")
-    if shape[-1] != cols or (cols > 1 and w.stride(-1) != 1):
+    if shape[-1] != cols or (stride[-1] != 1 and cols > 1):
         raise ValueError("weights are [cols] or [groups, cols], the last axis contiguous")
     if len(shape) == 1:
         return 0, cols, _dtype_code(w)
-    if len(shape) != 2 or x.dim() < 2 or shape[0] != x.shape[0]:
+    if len(shape) != 2 or len(xshape) < 2 or shape[0] != xshape[0]:
         raise ValueError("weights of a group of rows are [x.shape[0], cols]")
     groups = shape[0]
     per = x.numel() // (cols * groups) if groups and cols else 0
-    return (0 if groups == 1 else per), w.stride(0), _dtype_code(w)
+    return (0 if groups == 1 else per), stride[0], _dtype_code(w)
 
 
-def _statistics(x, rows, mean, rstd):
-    for t in (mean, rstd):
-        if t is not None and (t.numel() != rows or not t.is_contiguous() or _dtype_code(t) != FP32):
-            raise ValueError("mean and rstd: contiguous fp32, one element for each row of x")
+def _statistics(rows, device, *tensors):
+    for t in tensors:
+        if t is not None and (t.numel() != rows or _dtype_code(t) != FP32 or not t.is_contiguous() or t.get_device() != device):
+            raise ValueError("mean and rstd: contiguous fp32 on the current device, one element for each row of x")
 
 
 def layer_norm(x, weight, bias, y, mean=None, rstd=None, eps=1e-6, unit_offset=False, stream=None):
@@ -476,15 +477,20 @@ def layer_norm(x, weight, bias, y, mean=None, rstd=None, eps=1e-6, unit_offset=F
 
     weight, bias: None, [cols], or [x.shape[0], cols] (one row per sample).  mean, rstd: None or fp32 [...] to be
     written for layer_norm_backward.  y may be x."""
-    if y.shape != x.shape or y.dtype != x.dtype:
+    shape = x.shape
+    if y.shape != shape or y.dtype != x.dtype:
         raise ValueError("x and y must match")
-    sx, sy, cols = _row_stride(x, "x"), _row_stride(y, "y"), x.shape[-1]
+    cols = shape[-1]
+    sx = cols if x.is_contiguous() else _row_stride(x, "x")
+    sy = cols if y.is_contiguous() else _row_stride(y, "y")
     rows = x.numel() // cols if cols else 0
-    _statistics(x, rows, mean, rstd)
     per, sw, wcode = _norm_weights(x, weight, bias)
-    _here(x, y, weight, bias, mean, rstd)
-    status = lib().hilberta_layer_norm(x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), _ptr(mean), _ptr(rstd), rows, cols, per, sx,
-                                       sy, sw, _dtype_code(x), wcode, 1 if unit_offset else 0, eps, _stream_ptr(stream))
+    _here(x, y, weight, bias)
+    _statistics(rows, x.get_device(), mean, rstd)
+    status = lib().hilberta_layer_norm(x.data_ptr(), None if weight is None else weight.data_ptr(), None if bias is None else bias.data_ptr(),
+                                       y.data_ptr(), None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr(),
+                                       rows, cols, per, sx, sy, sw, _dtype_code(x), wcode, 1 if unit_offset else 0, eps,
+                                       _current_stream_ptr() if stream is None else int(stream.cuda_stream))
     if status:
         _check(status, "hilberta_layer_norm")
     return y, mean, rstd
@@ -499,30 +505,33 @@ def layer_norm_workspace(x, weight=None) -> int:
 def layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, unit_offset=False, workspace=None, stream=None):
     """Gradients of layer_norm into dx, dweight, dbias (any may be None, not all).  workspace: None (taken from torch's
     allocator) or a uint8 tensor of layer_norm_workspace() bytes."""
-    if dy.shape != x.shape or dy.dtype != x.dtype or (dx is not None and (dx.shape != x.shape or dx.dtype != x.dtype)):
+    shape, dtype = x.shape, x.dtype
+    if dy.shape != shape or dy.dtype != dtype or (dx is not None and (dx.shape != shape or dx.dtype != dtype)):
         raise ValueError("dy, x and dx must match")
     if mean is None or rstd is None:
         raise ValueError("mean and rstd of the forward pass are needed")
-    sdy, sx, cols = _row_stride(dy, "dy"), _row_stride(x, "x"), x.shape[-1]
-    sdx = 0 if dx is None else _row_stride(dx, "dx")
+    cols = shape[-1]
+    sx = cols if x.is_contiguous() else _row_stride(x, "x")
+    sdy = cols if dy.is_contiguous() else _row_stride(dy, "dy")
+    sdx = cols if dx is None or dx.is_contiguous() else _row_stride(dx, "dx")
     rows = x.numel() // cols if cols else 0
-    _statistics(x, rows, mean, rstd)
     per, sw, wcode = _norm_weights(x, weight, None)
-    sdw = 0
+    L, sdw, ws_bytes = lib(), 0, 0
     if dweight is not None or dbias is not None:
         gper, sdw, gcode = _norm_weights(x, dweight, dbias)
         if weight is not None and (gper != per or gcode != wcode):
             raise ValueError("a weight and its gradient: one shape and dtype")
         per, wcode = gper, gcode
         if workspace is None:
-            n = lib().hilberta_layer_norm_workspace(rows, cols, per)
-            if n:
-                workspace = _scratch(n, x, stream)
-    _here(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace)
-    status = lib().hilberta_layer_norm_backward(dy.data_ptr(), x.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(), _ptr(dx),
-                                                _ptr(dweight), _ptr(dbias), _ptr(workspace), 0 if workspace is None else workspace.nbytes,
-                                                rows, cols, per, sdy, sx, sdx, sw, sdw, _dtype_code(x), wcode, 1 if unit_offset else 0,
-                                                _stream_ptr(stream))
+            ws_bytes = L.hilberta_layer_norm_workspace(rows, cols, per)
+            if ws_bytes:
+                workspace = _scratch(ws_bytes, x, stream)
+    _here(x, dy, weight, dx, dweight, dbias, workspace)
+    _statistics(rows, x.get_device(), mean, rstd)
+    status = L.hilberta_layer_norm_backward(dy.data_ptr(), x.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(), _ptr(dx),
+                                            _ptr(dweight), _ptr(dbias), _ptr(workspace), 0 if workspace is None else ws_bytes or workspace.nbytes,
+                                            rows, cols, per, sdy, sx, sdx, sw, sdw, _dtype_code(x), wcode, 1 if unit_offset else 0,
+                                            _stream_ptr(stream))
     if status:
         _check(status, "hilberta_layer_norm_backward")
     return dx, dweight, dbias
@@ -545,21 +554,28 @@ def _rotary(fn, name, x, out, inv_freq, positions, axis, interleaved, factor, pl
         import torch
         _host_types.extend((torch.float64, torch.int32))
     f64, int32 = _host_types
-    shape, sx, so = x.shape, x.stride(), out.stride()
-    if len(shape) != 4 or out.shape != shape or out.dtype != x.dtype:
+    shape, dtype = x.shape, x.dtype
+    if len(shape) != 4 or out.shape != shape or out.dtype != dtype:
         raise ValueError("x and out: [batch, heads, S, head_dim], one shape and dtype")
     B, H, S, D = shape
-    if D > 1 and (sx[3] != 1 or so[3] != 1):
+    xb, xh, xs, xd = x.stride()
+    ob, oh, os_, od = out.stride()
+    if (xd != 1 or od != 1) and D > 1:
         raise ValueError("the head_dim axis has to be contiguous")
-    if inv_freq.dtype != f64 or inv_freq.is_cuda or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+    if inv_freq.dtype != f64 or inv_freq.dim() != 1 or inv_freq.is_cuda or not inv_freq.is_contiguous():
         raise ValueError("inv_freq: contiguous fp64 [pairs] on the CPU")
-    axes, pos_stride = 1, 0
+    axes, pos_stride, pos = 1, 0, None
     if axis is not None and (axis.dtype != int32 or axis.is_cuda or axis.shape != inv_freq.shape or not axis.is_contiguous()):
         raise ValueError("axis: contiguous int32 [pairs] on the CPU")
+    device = _current_device()
+    if x.get_device() != device or out.get_device() != device:
+        _here(x, out)
     if positions is not None:
         if positions.dtype != int32 or not positions.is_contiguous():
             raise ValueError("positions: contiguous int32")
-        ps = tuple(positions.shape)
+        if positions.get_device() != device:
+            _here(positions)
+        ps = positions.shape
         if axis is not None:
             if not ps:
                 raise ValueError("positions: [S, axes] or [batch, S, axes]")
@@ -568,10 +584,10 @@ def _rotary(fn, name, x, out, inv_freq, positions, axis, interleaved, factor, pl
             pos_stride = S
         elif ps != (S,):
             raise ValueError("positions: [S] or [batch, S], with an axis for each position axis if `axis` is given")
-    _here(x, out, positions)
-    status = fn(x.data_ptr(), out.data_ptr(), _ptr(positions), inv_freq.data_ptr(), _ptr(axis), inv_freq.numel(), axes,
+        pos = positions.data_ptr()
+    status = fn(x.data_ptr(), out.data_ptr(), pos, inv_freq.data_ptr(), None if axis is None else axis.data_ptr(), inv_freq.numel(), axes,
                 1 if interleaved else 0, factor, None if plan is None else plan._h, B, H, S, D, _dtype_code(x),
-                _I64x6(sx[0], sx[1], sx[2], so[0], so[1], so[2]), pos_stride, _stream_ptr(stream))
+                _I64x6(xb, xh, xs, ob, oh, os_), pos_stride, _current_stream_ptr() if stream is None else int(stream.cuda_stream))
     if status:
         _check(status, name)
     return out
@@ -591,7 +607,7 @@ def rotary_backward(dout, dx, inv_freq, positions=None, axis=None, interleaved=F
 
 
 def _packed_args(like_q, like_k, lse, cu_seqlens):
-    """(total, heads, kv_heads, head_dim) of packed tensors, those of q's shape and those of k's, and their strides."""
+    """(total, heads, kv_heads, head_dim) of packed tensors, those of q's shape and those of k's, and all their strides."""
     if not _host_types:
         import torch
         _host_types.extend((torch.float64, torch.int32))
@@ -600,27 +616,30 @@ def _packed_args(like_q, like_k, lse, cu_seqlens):
     if len(qs) != 3 or len(ks) != 3 or qs[0] != ks[0] or qs[2] != ks[2]:
         raise ValueError("packed tensors are [total, heads, head_dim] and [total, kv_heads, head_dim]")
     T, H, D = qs
-    device = _current_device()
+    Hk, device = ks[1], _current_device()
     for ts, shape in ((like_q, qs), (like_k, ks)):
         for t in ts:
             if t.shape != shape or t.dtype != dtype:
                 raise ValueError("packed tensors must match: one shape for q's kind and one for k's, one dtype")
-            st, sh, sd = t.stride()
-            if sd != 1 and D > 1:
-                raise ValueError("the head_dim axis has to be contiguous")
             if t.get_device() != device:
-                raise ValueError(f"tensor on {t.device}, the current device is cuda:{device}")
-            if shape[1] == 1:   # an axis of one element has any stride
-                sh = (D + 7) // 8 * 8
+                _here(t)
+            strides += t.stride()
+    if D > 1 and strides[2::3].count(1) * 3 != len(strides):
+        raise ValueError("the head_dim axis has to be contiguous")
+    if T <= 1 or H == 1 or Hk == 1:   # an axis of one element has any stride
+        for i in range(0, len(strides), 3):
+            heads = H if i < 3 * len(like_q) else Hk
+            if heads == 1:
+                strides[i + 1] = (D + 7) // 8 * 8
             if T <= 1:
-                st = max(shape[1] * sh, 8)
-            strides += (st, sh)
-    if lse is not None and (lse.shape != (H, T) or not lse.is_contiguous() or _dtype_code(lse) != FP32):
-        raise ValueError("lse: contiguous fp32 [heads, total]")
+                strides[i] = max(heads * strides[i + 1], 8)
+    if lse is not None and (lse.shape != (H, T) or _dtype_code(lse) != FP32 or not lse.is_contiguous() or lse.get_device() != device):
+        raise ValueError("lse: contiguous fp32 [heads, total] on the current device")
     if cu_seqlens.dtype != _host_types[1] or cu_seqlens.dim() != 1 or not cu_seqlens.is_contiguous() or cu_seqlens.numel() < 1:
         raise ValueError("cu_seqlens: contiguous int32 [sequences + 1]")
-    _here(lse, cu_seqlens)
-    return T, H, ks[1], D, strides
+    if cu_seqlens.get_device() != device:
+        _here(cu_seqlens)
+    return T, H, Hk, D, strides
 
 
 def packed_forward(q, k, v, out, cu_seqlens, lse=None, causal=True, scale=0.0, stream=None):
@@ -629,7 +648,7 @@ def packed_forward(q, k, v, out, cu_seqlens, lse=None, causal=True, scale=0.0, s
     T, H, Hk, D, st = _packed_args((q, out), (k, v), lse, cu_seqlens)
     status = lib().hilberta_packed_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse), cu_seqlens.data_ptr(),
                                            cu_seqlens.numel() - 1, T, H, Hk, D, _dtype_code(q),
-                                           _I64x8(st[0], st[1], st[4], st[5], st[6], st[7], st[2], st[3]), 1 if causal else 0, scale,
+                                           _I64x8(st[0], st[1], st[6], st[7], st[9], st[10], st[3], st[4]), 1 if causal else 0, scale,
                                            _stream_ptr(stream))
     if status:
         _check(status, "hilberta_packed_forward")
@@ -654,8 +673,8 @@ def packed_backward(dout, q, k, v, out, lse, dq, dk, dv, cu_seqlens, causal=True
     status = lib().hilberta_packed_backward(dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
                                             dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), workspace.data_ptr(), workspace.nbytes,
                                             cu_seqlens.data_ptr(), cu_seqlens.numel() - 1, T, H, Hk, D, _dtype_code(q),
-                                            _I64x16(st[0], st[1], st[2], st[3], st[8], st[9], st[10], st[11], st[4], st[5], st[6], st[7],
-                                                    st[12], st[13], st[14], st[15]), 1 if causal else 0, scale, _stream_ptr(stream))
+                                            _I64x16(st[0], st[1], st[3], st[4], st[12], st[13], st[15], st[16], st[6], st[7],
+                                                    st[9], st[10], st[18], st[19], st[21], st[22]), 1 if causal else 0, scale, _stream_ptr(stream))
     if status:
         _check(status, "hilberta_packed_backward")
     return dq, dk, dv
