@@ -34,6 +34,7 @@ constexpr int SLAB_BYTES = BN * 128;     // 64 columns of 128 rows
 constexpr int THREADS = 384;
 constexpr uint32_t TMEM_COLS = 512;
 constexpr float RESCALE_THRESHOLD = 8.0f;   // log2: the reference maximum moves only when a score exceeds it by 2^8
+constexpr int POLY_DEG = 4;              // of the exponentials on the FMA pipes: lse keeps six digits (TIMED)
 constexpr int SPLIT_AT = 2;              // P goes to the MMA issuer as the keys of 32-key chunks 0 .. 2, then the rest
 __host__ __device__ constexpr int tile_bytes(int hd) { return BN * hd * 2; }
 __host__ __device__ constexpr int smem_bytes(int hd) { return (QT + ring_slots(hd)) * tile_bytes(hd) + STAGE_BYTES + 1024; }
@@ -435,7 +436,7 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                     // The row sum is taken over the fp32 weights, the MMA sees them in bf16: the rounding error of the
                     // block's largest weight, computed exactly as below, goes into the output's normaliser.
                     const float xm = fmaf(mx_raw, scale_log2, -m_ref);
-                    const float pm_fma = ex2_poly1<HB_POLY_DEG>(xm);
+                    const float pm_fma = ex2_poly1<POLY_DEG>(xm);
                     const float pm = top_on_fma ? pm_fma : ex2(xm);
                     l_fix += __uint_as_float(pack_bf16(0.f, pm) & 0xffff0000u) - pm;
                 }
@@ -448,7 +449,7 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                                                     sc2, nm2);
                         float2 p;
                         if ((i & HB_POLY_MASK) == HB_POLY_MASK) {
-                            p = ex2_poly2<HB_POLY_DEG>(x);
+                            p = ex2_poly2<POLY_DEG>(x);
                         } else {
                             p.x = ex2(x.x);
                             p.y = ex2(x.y);

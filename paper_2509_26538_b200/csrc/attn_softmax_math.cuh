@@ -36,6 +36,11 @@ __device__ __forceinline__ float2 ex2_poly2(float2 x) {
     if constexpr (DEG == 2) {
         p = __ffma2_rn(f, make_float2(0.23842697f, 0.23842697f), make_float2(0.7034453f, 0.7034453f));
         p = __ffma2_rn(p, f, make_float2(1.00044307f, 1.00044307f));
+    } else if constexpr (DEG == 4) {   // 2.7e-6, for a row sum whose logarithm is handed out
+        p = __ffma2_rn(f, make_float2(0.00957010195f, 0.00957010195f), make_float2(0.0559178616f, 0.0559178616f));
+        p = __ffma2_rn(p, f, make_float2(0.240247448f, 0.240247448f));
+        p = __ffma2_rn(p, f, make_float2(0.693121815f, 0.693121815f));
+        p = __ffma2_rn(p, f, make_float2(0.999999261f, 0.999999261f));
     } else {
         p = __ffma2_rn(f, make_float2(0.055088773f, 0.055088773f), make_float2(0.24260406f, 0.24260406f));
         p = __ffma2_rn(p, f, make_float2(0.69327623f, 0.69327623f));
@@ -58,6 +63,11 @@ __device__ __forceinline__ float ex2_poly1(float x) {
     if constexpr (DEG == 2) {
         p = __fmaf_rn(f, 0.23842697f, 0.7034453f);
         p = __fmaf_rn(p, f, 1.00044307f);
+    } else if constexpr (DEG == 4) {
+        p = __fmaf_rn(f, 0.00957010195f, 0.0559178616f);
+        p = __fmaf_rn(p, f, 0.240247448f);
+        p = __fmaf_rn(p, f, 0.693121815f);
+        p = __fmaf_rn(p, f, 0.999999261f);
     } else {
         p = __fmaf_rn(f, 0.055088773f, 0.24260406f);
         p = __fmaf_rn(p, f, 0.69327623f);
