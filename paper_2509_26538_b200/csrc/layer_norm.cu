@@ -143,12 +143,16 @@ layer_norm_kernel(const ForwardParams prm) {
         if (in && col(i) < cols) v[i].load(x + col(i));
         else v[i].zero();
     }
-    auto pair = [&](int i, int e) { return VEC > 1 ? v[i].pair(e) : make_float2(v[i].get(0), v[(i + 1) % NV].get(0)); };
-    float2 acc[2] = {both(0.f), both(0.f)};   // two chains
+    // unpacked once: in bf16 that is what the integer pipe, the busiest one, spends its time on
+    float2 d[NV / STEP * P], acc[2] = {both(0.f), both(0.f)};   // two chains
 #pragma unroll
     for (int i = 0; i < NV; i += STEP)
 #pragma unroll
-        for (int e = 0; e < P; ++e) acc[(i + e) & 1] = __fadd2_rn(acc[(i + e) & 1], pair(i, e));
+        for (int e = 0; e < P; ++e) {
+            float2 &at = d[i / STEP * P + e];
+            at = VEC > 1 ? v[i].pair(e) : make_float2(v[i].get(0), v[(i + 1) % NV].get(0));
+            acc[(i + e) & 1] = __fadd2_rn(acc[(i + e) & 1], at);
+        }
     acc[0] = __fadd2_rn(acc[0], acc[1]);
     const float mean = row_sum(acc[0].x + acc[0].y, 0) / (float)cols;
     const float2 shift = both(-mean);
@@ -158,9 +162,10 @@ layer_norm_kernel(const ForwardParams prm) {
         if (col(i) < cols) {
 #pragma unroll
             for (int e = 0; e < P; ++e) {
-                float2 d = __fadd2_rn(pair(i, e), shift);
-                if (VEC == 1 && col(i + 1) >= cols) d.y = 0.f;
-                acc[(i + e) & 1] = __ffma2_rn(d, d, acc[(i + e) & 1]);
+                float2 &at = d[i / STEP * P + e];
+                at = __fadd2_rn(at, shift);
+                if (VEC == 1 && col(i + 1) >= cols) at.y = 0.f;
+                acc[(i + e) & 1] = __ffma2_rn(at, at, acc[(i + e) & 1]);
             }
         }
     }
@@ -191,7 +196,7 @@ layer_norm_kernel(const ForwardParams prm) {
         if (col(i) >= cols) continue;
         float2 f[P], t[P];
 #pragma unroll
-        for (int e = 0; e < P; ++e) f[e] = __fmul2_rn(__fadd2_rn(pair(i, e), shift), scale);
+        for (int e = 0; e < P; ++e) f[e] = __fmul2_rn(d[i / STEP * P + e], scale);
         if (w) {
             weights(t, w, i);
 #pragma unroll
@@ -588,15 +593,15 @@ layer_norm_bwd_kernel(const BackwardParams prm) {
     }
 }
 
-// dw, db of a group: the sums of its CTAs added up in a fixed order.  32 columns a block; SUMS rows of threads
-// share the CTAs out.
-constexpr int SUMS = 32;
-template <class W>
-__global__ void __launch_bounds__(32 * SUMS)
+// dw, db of a group: the sums of its CTAs added up in a fixed order.  16 columns a block (64 bytes of each CTA's); SUMS rows of
+// threads share the CTAs out: 64 for many, 16 where more would only wait.
+constexpr int SUM_COLS = 16;
+template <class W, int SUMS>
+__global__ void __launch_bounds__(SUM_COLS * SUMS)
 layer_norm_sums_kernel(const float *partial, void *dweight, void *dbias, int cols, int ctas, long long stride_dw) {
-    __shared__ float part[SUMS][33];
-    const int lane = threadIdx.x % 32, slot = threadIdx.x / 32, which = blockIdx.z;
-    const int c = blockIdx.x * 32 + lane;
+    __shared__ float part[SUMS][SUM_COLS + 1];
+    const int lane = threadIdx.x % SUM_COLS, slot = threadIdx.x / SUM_COLS, which = blockIdx.z;
+    const int c = blockIdx.x * SUM_COLS + lane;
     allow_next();
     wait_for_previous();
     void *to = which ? dbias : dweight;
@@ -609,13 +614,19 @@ layer_norm_sums_kernel(const float *partial, void *dweight, void *dbias, int col
     }
     part[slot][lane] = sum;
     __syncthreads();
-    if (slot == 0 && c < cols) {
-        sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < SUMS; ++i) sum += part[i][lane];
-        Vec<W, 1> o;
-        o.set(&sum);
-        o.store((W *)to + blockIdx.y * stride_dw + c);
+    // LANES lanes for each column
+    constexpr int LANES = SUMS < 32 ? SUMS : 32;
+    const int col = threadIdx.x / LANES, k = threadIdx.x % LANES;
+    if (col < SUM_COLS) {   // whole warps
+        sum = part[k][col];
+        if (SUMS > 32) sum += part[k + SUMS / 2][col];
+        sum = lanes_sum<LANES>(sum);
+        const int out = blockIdx.x * SUM_COLS + col;
+        if (k == 0 && out < cols) {
+            Vec<W, 1> o;
+            o.set(&sum);
+            o.store((W *)to + blockIdx.y * stride_dw + out);
+        }
     }
 }
 
@@ -703,7 +714,7 @@ struct BackwardShape {
     long long round() const { return lanes ? (long long)r * (256 / lanes) : (long long)r * teams; }   // rows of a round
 };
 
-BackwardShape backward_shape(const Shape &s, bool aligned) {
+BackwardShape backward_shape(const Shape &s, bool aligned, int sms) {
     BackwardShape g{};
     if (s.cols <= 256 && (aligned || s.cols <= 32)) {
         g.lanes = s.cols <= 8 * 8 && aligned ? 8 : 32;
@@ -738,6 +749,7 @@ BackwardShape backward_shape(const Shape &s, bool aligned) {
     const int limit = (g.warps == MAX_WARPS ? 200 : 110) << 10;
     while (g.r > 1 && 3 * 2 * g.r * g.teams * g.pitch > limit) g.r /= 2;
     while (g.teams > 1 && 3 * 2 * g.r * g.teams * g.pitch > limit) --g.teams;
+    // few rows: on all SMs
     return g;
 }
 
@@ -774,7 +786,6 @@ int launch_backward(BackwardCall &c) {
     static std::atomic<uint64_t> opted{0};
     if (!(opted.load() >> c.device & 1)) {
         HB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 << 10));
-        HB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 100));
         opted.fetch_or(1ull << c.device);
     }
     const int threads = 32 * (g.warps * g.teams + 1), stage = 2 * g.r * g.teams * g.pitch;
@@ -898,7 +909,7 @@ extern "C" size_t hilberta_layer_norm_workspace(int64_t rows, int cols, int64_t 
     for (size_t esz : {2, 4})   // whatever the type and the alignment
         for (bool aligned : {false, true}) {
             s.esz = esz;
-            const BackwardShape g = backward_shape(s, aligned);
+            const BackwardShape g = backward_shape(s, aligned, sms);
             ctas = std::max(ctas, std::min((s.rows_per_group + g.round() - 1) / g.round(), (long long)sms * MAX_PER_SM / std::max(1ll, s.groups)));
         }
     return ctas > 1 ? (size_t)(ctas * s.groups) * 2 * (size_t)cols * sizeof(float) : 0;
@@ -940,7 +951,7 @@ extern "C" int hilberta_layer_norm_backward(const void *dy, const void *x, const
                          aligned16(weight, prm.stride_w, s.wsz) && aligned16(dweight, prm.stride_dw, s.wsz) &&
                          aligned16(dbias, prm.stride_dw, s.wsz);
     BackwardCall c{};
-    c.g = backward_shape(s, vectors);
+    c.g = backward_shape(s, vectors, sms);
     prm.team_warps = c.g.warps;
     prm.pitch = c.g.pitch;
     c.prm = prm;
@@ -958,8 +969,10 @@ extern "C" int hilberta_layer_norm_backward(const void *dy, const void *x, const
         using W = decltype(w);
         const int rc2 = backward_by_cols<T, W>(c, vectors);
         if (rc2 != HILBERTA_OK || !c.sums) return rc2;
-        HB_CUDA(launch_overlapping(layer_norm_sums_kernel<W>, dim3((unsigned)((cols + 31) / 32), (unsigned)s.groups, 2), 32 * SUMS, 0, 1, st,
-                                   true, (const float *)c.prm.partial, dweight, dbias, cols, (int)c.ctas, (long long)prm.stride_dw));
+        const bool many = c.ctas > 128;
+        HB_CUDA(launch_overlapping(many ? layer_norm_sums_kernel<W, 64> : layer_norm_sums_kernel<W, 16>,
+                                   dim3((unsigned)((cols + SUM_COLS - 1) / SUM_COLS), (unsigned)s.groups, 2), SUM_COLS * (many ? 64 : 16), 0, 1,
+                                   st, true, (const float *)c.prm.partial, dweight, dbias, cols, (int)c.ctas, (long long)prm.stride_dw));
         HB_LAUNCHED();
         return HILBERTA_OK;
     });

@@ -153,7 +153,7 @@ __device__ __forceinline__ float turned(float x, float partner, float cs, float 
 // interleaved one -- of heads_per_thread heads of one token, HU of them in flight; further threads of the row copy
 // what is not rotated, 16 bytes each.
 template <class T, bool INTERLEAVED, int HU>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, 6)
 rotary_kernel(const __grid_constant__ Params p, const Divider per_batch, const Divider per_row) {
     constexpr int N = 16 / (int)sizeof(T);   // pairs of a thread = elements of a run
     __shared__ Table table;
