@@ -642,6 +642,16 @@ bool rows_overlap(const void *a, long long sa, const void *b, long long sb, long
     return a0 < b0 + lb && b0 < a0 + la;
 }
 
+// Do `rows` rows of cols elements, stride apart, share a byte with as many at b?  (Two slices of one tensor may lie side by side.)
+bool slices_overlap(const void *a, const void *b, long long stride, long long rows, int cols, size_t esz) {
+    if (!a || !b || rows < 1) return false;
+    const uintptr_t lo = std::min((uintptr_t)a, (uintptr_t)b), d = std::max((uintptr_t)a, (uintptr_t)b) - lo;
+    const uintptr_t row = (uintptr_t)cols * esz, step = rows > 1 ? (uintptr_t)stride * esz : 0;
+    if (rows == 1 || step == 0) return d < row;
+    if (d >= (uintptr_t)(rows - 1) * step + row) return false;
+    return d % step < row || d % step + row > step;
+}
+
 struct Shape {
     long long rows, rows_per_group, groups;
     int cols, dtype, weight_dtype;
@@ -884,6 +894,7 @@ extern "C" int hilberta_layer_norm(const void *x, const void *weight, const void
         ((uintptr_t)mean | (uintptr_t)rstd) & 3)
         return HILBERTA_ERR_INVALID;
     if (s.groups > 1 && (weight || bias) && stride_w < 0) return HILBERTA_ERR_INVALID;
+    if (mean && mean == rstd) return HILBERTA_ERR_INVALID;
     if (rows_overlap(x, stride_x, y, stride_y, rows, cols, s.esz)) return HILBERTA_ERR_INVALID;
     int dev = -1;
     HB_CUDA(cudaGetDevice(&dev));
@@ -936,6 +947,7 @@ extern "C" int hilberta_layer_norm_backward(const void *dy, const void *x, const
     if (rows_overlap(dx, stride_dx, x, stride_x, rows, cols, s.esz) || rows_overlap(dx, stride_dx, dy, stride_dy, rows, cols, s.esz))
         return HILBERTA_ERR_INVALID;
     if (s.groups > 65535) return HILBERTA_ERR_UNSUPPORTED;
+    if (slices_overlap(dweight, dbias, stride_dw, std::max(s.groups, 1ll), cols, s.wsz)) return HILBERTA_ERR_INVALID;
     int dev = -1;
     HB_CUDA(cudaGetDevice(&dev));
     const int sms = sm100_count(dev);

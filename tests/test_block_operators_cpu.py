@@ -51,6 +51,25 @@ def test_layer_norm_backward_refuses(lib, bad, status):
     assert _norm_grad(lib, **bad) == status
 
 
+@pytest.mark.parametrize("bad", [
+    dict(dw=4 * PTR, db=4 * PTR), dict(dw=4 * PTR, db=4 * PTR + 252), dict(per=2, dw=4 * PTR, db=4 * PTR + 128, sdw=96),
+    dict(per=2, dw=4 * PTR + 256, db=4 * PTR, sdw=64), dict(per=1, sdw=128, dw=4 * PTR + 3 * 512 + 4, db=4 * PTR),
+])
+def test_layer_norm_backward_refuses_gradients_that_overlap(lib, bad):
+    assert _norm_grad(lib, **{"ws": PTR, "ws_bytes": 1 << 30, **bad}) == hb.ERR_INVALID
+
+
+def test_layer_norm_backward_takes_gradients_side_by_side(lib):
+    if torch.cuda.is_available():
+        pytest.skip("would launch on made-up pointers")
+    for ok in (dict(dw=4 * PTR, db=4 * PTR + 256), dict(per=2, dw=4 * PTR + 256, db=4 * PTR, sdw=128), dict(per=1, sdw=192, dw=4 * PTR, db=4 * PTR + 512)):
+        assert _norm_grad(lib, ws=PTR, ws_bytes=1 << 30, **ok) == hb.ERR_CUDA
+
+
+def test_statistics_have_a_place_each(lib):
+    assert _norm(lib, mean=PTR, rstd=PTR) == hb.ERR_INVALID
+
+
 def _rotary(lib, fn="hilberta_rotary", x=PTR, out=2 * PTR, pos=None, freq=None, axis=None, pairs=32, axes=1, factor=1.0, plan=None, batch=1,
             heads=2, S=5, dim=64, dtype=hb.BF16, strides=(640, 320, 64, 640, 320, 64), no_freq=False):
     f = np.ones(max(pairs, 1)) if freq is None else np.asarray(freq, dtype=np.float64)
