@@ -451,6 +451,8 @@ int hilberta_packed_forward(const void *q, const void *k, const void *v, void *o
  *   strides       (token, head) of dout, q, k, v, out, dq, dk, dv in turn.
  *   workspace     hilberta_packed_workspace(total, heads) bytes of device memory, 16-byte aligned, which the call
  *                 overwrites; calls that may overlap on the device need one each.  ERR_BUFFER if it is too small.
+ *                 The bytes are those for the current device: two floats a row and head, and up to 160 MB of partial
+ *                 sums where `total` is small next to the device.
  * Every sum is taken in a fixed order: the same call gives the same bits. */
 int hilberta_packed_backward(const void *dout, const void *q, const void *k, const void *v, const void *out, const float *lse,
                              void *dq, void *dk, void *dv, void *workspace, size_t workspace_bytes, const int32_t *cu_seqlens,

@@ -656,7 +656,7 @@ def packed_forward(q, k, v, out, cu_seqlens, lse=None, causal=True, scale=0.0, s
 
 
 def packed_workspace(total, heads) -> int:
-    """Bytes of workspace that packed_backward needs."""
+    """Bytes of workspace that packed_backward needs on the current device."""
     return int(lib().hilberta_packed_workspace(int(total), int(heads)))
 
 

@@ -1,11 +1,11 @@
 // Gradients of the attention over packed sequences, for sm_100a.  With P = exp(s q k^T - lse), dP = dO V^T,
 // delta = rowsum(dO * O) and dS = P * (dP - delta):   dQ = s dS K,   dK = s dS^T Q,   dV = P^T dO.
 //
-// Two launches: a bandwidth-bound pass that leaves (lse log2 e, delta) of every row in the workspace, then one
-// tensor-core kernel whose CTAs work in one of two modes:
+// Two launches, three where key tiles are few (key_splits): a bandwidth-bound pass that leaves (lse log2 e, delta) of every
+// row in the workspace, then one tensor-core kernel whose CTAs work in one of two modes:
 //   mode DQ    resident tile = 128 query rows (Q_i, dO_i: 128 / g tokens of g heads, see the forward kernel),
 //              streamed = their keys (K_j, V_j):   A = Q_i K_j^T, B = dO_i V_j^T, dS -> TMEM, dQ_i += dS K_j
-//   mode DKV   resident tile = 128 keys (K_j, V_j), streamed = the query rows of all heads of the group that see them:
+//   mode DKV   resident tile = 128 keys (K_j, V_j), streamed = the query rows of the group's heads (or of a part of them) that see them:
 //              A = K_j Q_i^T, B = V_j dO_i^T (a thread owns a KEY row), P^T, dS^T -> TMEM, dV_j += P^T dO_i, dK_j += dS^T Q_i
 // Seven products where one pass that adds dQ up in memory would take five, but no atomics: every sum is taken in a
 // fixed order, the heads of a group among them, and no fp32 copy of dQ is written and read.
@@ -16,8 +16,8 @@
 // Bound by the chain dP -> phase 2 -> output products -> next dP: 2.1 us a block in DKV mode (four products, 1.5 at the matrix
 // rate of a large library product), 1.4 in DQ mode (three, 1.1); tensor pipe 61 % of the cycles.  Measured (B200, us): four
 // documents of 333 ... 4096 tokens, 16 heads over 4 key heads, causal, head dim 128: 300 (statistics 15 of it), with each mode's
-// CTAs and their units fixed beforehand 379.  Few short prompts are as long as their longest key tile: 38 for eight of 1 ... 511
-// tokens, three heads to a key head (12 blocks one after the other, 25).
+// CTAs and their units fixed beforehand 379.  Few short prompts: 35 for eight of 1 ... 511 tokens, three heads to a key head, 30 of it
+// 336 units of one to four blocks on 148 SMs.
 // Per block the tensor pipe sees  A(s+1) | out(s) | B(s+1)  back to back: the element-wise step turns scores into
 // weights as soon as A is written (phase 1) and frees A for the next block; phase 2 overwrites B in place with P and dS.
 #include <algorithm>
@@ -71,6 +71,9 @@ __device__ int g_status[64];
 struct Params {
     packed::Sequences queries, keys;   // blocks of a DQ unit (128 / g tokens) and of a DKV unit (128 tokens)
     int kv_heads, odd, group, g_shift, heads;   // group = odd << g_shift
+    // DKV: the group's heads in `splits` parts of k_odd << k_shift, a unit each; more than one part leaves partial sums
+    int splits, k_odd, k_shift;
+    float *partial;   // [splits, 2 (dk, dv), total, kv_heads, head_dim], nullptr with one part
     unsigned dkv_units;   // CTAs of the launch that stand for units of the DKV mode
     const float *lse2, *delta;   // [total, heads]
     __nv_bfloat16 *dq, *dk, *dv;
@@ -104,10 +107,10 @@ __device__ __forceinline__ Work work_of(const Params &p, const packed::Unit &u) 
         // a causal level counts from the block with the fewest queries, the last one
         const int b = p.keys.causal ? blocks - 1 - u.block : u.block;
         w.tok0 = b * BM;
-        w.kv_head = u.head;
-        w.head0 = u.head * p.group;
-        w.first = p.keys.causal ? b << p.g_shift : 0;
-        w.count = (int)((((long long)w.len << p.g_shift) + BK - 1) / BK) - w.first;
+        w.kv_head = u.head / p.splits;
+        w.head0 = w.kv_head * p.group + (u.head % p.splits) * (p.k_odd << p.k_shift);
+        w.first = p.keys.causal ? b << p.k_shift : 0;
+        w.count = (int)((((long long)w.len << p.k_shift) + BK - 1) / BK) - w.first;
     }
     return w;
 }
@@ -147,6 +150,7 @@ template <int HD>
 __global__ void __launch_bounds__(THREADS, 1)
 packed_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                   const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmdO,
+                  const __grid_constant__ CUtensorMap tmQs, const __grid_constant__ CUtensorMap tmdOs,   // as DKV streams them
                   const __grid_constant__ Params prm) {
     extern __shared__ uint8_t smem_raw[];
     constexpr uint32_t REG_A = 0, REG_B = 128, OUT_A = 256, OUT_B = 384;   // TMEM columns
@@ -225,11 +229,12 @@ packed_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             bool ok = true;
             auto stream = [&](auto mode, const packed::Unit &u) {
                 constexpr int MODE = decltype(mode)::value;
-                const CUtensorMap *tm = MODE == MODE_DKV ? (second ? &tmdO : &tmQ) : (second ? &tmV : &tmK);
+                const CUtensorMap *tm = MODE == MODE_DKV ? (second ? &tmdOs : &tmQs) : (second ? &tmV : &tmK);
+                const int g_shift = prm.k_shift;   // of the streamed rows, DKV
                 const int tps = MODE == MODE_DKV ? BK >> g_shift : BK;   // tokens of a streamed block
                 const Work w = work_of<MODE>(prm, u);
                 // head parts that are streamed one after the other
-                for (int rep = 0; ok && rep < (MODE == MODE_DKV ? prm.odd : 1); ++rep) {
+                for (int rep = 0; ok && rep < (MODE == MODE_DKV ? prm.k_odd : 1); ++rep) {
                     const int head = MODE == MODE_DKV ? w.head0 + (rep << g_shift) : w.kv_head;
                     for (int j = 0; j < w.count; ++j, ++g) {
                         const int tok = (w.first + j) * tps;
@@ -288,6 +293,8 @@ packed_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             prefetch_tmap(&tmK);
             prefetch_tmap(&tmV);
             prefetch_tmap(&tmdO);
+            prefetch_tmap(&tmQs);
+            prefetch_tmap(&tmdOs);
         }
         packed::Runs key_runs, query_runs;
         const packed::Span key_span = packed::span_of(prm.keys, lane), query_span = packed::span_of(prm.queries, lane);
@@ -297,7 +304,7 @@ packed_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         bool more = true, ok = true;
         auto find = [&](packed::Unit &u) {
             u.mode = n < prm.dkv_units ? MODE_DKV : MODE_DQ;
-            return n < prm.dkv_units ? packed::find_unit(prm.keys, key_span, key_runs, prm.kv_heads, n, u)
+            return n < prm.dkv_units ? packed::find_unit(prm.keys, key_span, key_runs, prm.kv_heads * prm.splits, n, u)
                                      : packed::find_unit(prm.queries, query_span, query_runs, prm.kv_heads * prm.odd, n - prm.dkv_units, u);
         };
         auto ask_next = [&] {
@@ -384,7 +391,12 @@ packed_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     uint32_t o[32];
                     tmem_ld32(tmem + lane_addr + (c >= CPO ? OUT_B + (c - CPO) * 32 : OUT_A + c * 32), o);
                     tmem_wait_ld();
-                    if (tok < w.len) {
+                    if (tok < w.len && MODE == MODE_DKV && prm.partial) {
+                        const long long which = (u.head % prm.splits) * 2 + (c >= CPO ? 1 : 0);
+                        float *const to = prm.partial + ((which * prm.keys.total + row) * prm.kv_heads + head) * HD + (c % CPO) * 32;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4 *>(to + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                    } else if (tok < w.len) {
                         __nv_bfloat16 *orow = (c >= CPO ? out_b : out_a) + (c % CPO) * 32;
                         const float mul = c >= CPO ? 1.f : prm.scale;
                         uint32_t v[16];
@@ -416,7 +428,7 @@ packed_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             auto t2 = [&](uint32_t e) { return sT2 + (e % NT2) * TILE_BYTES; };
             auto multiply = [&](auto mode, const packed::Unit &u) {
                 constexpr int MODE = decltype(mode)::value;
-                const int n = work_of<MODE>(prm, u).count * (MODE == MODE_DKV ? prm.odd : 1);
+                const int n = work_of<MODE>(prm, u).count * (MODE == MODE_DKV ? prm.k_odd : 1);
                 ok = wait_or_abort(bar(RES_FULL), n_unit & 1, abort_flag, status, 0x501);
                 if (!ok) return;
                 // scores and dP of the first block
@@ -516,7 +528,7 @@ packed_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     row_l2 = __ldg(prm.lse2 + at);
                     row_dl = __ldg(prm.delta + at);
                 }
-                for (int rep = 0; ok && rep < (MODE == MODE_DKV ? prm.odd : 1); ++rep) {
+                for (int rep = 0; ok && rep < (MODE == MODE_DKV ? prm.k_odd : 1); ++rep) {
                     for (int j = 0; j < w.count; ++j, ++g) {
                         // Pairs that exist: streamed columns lo <= c < hi of this warpgroup's 64; dS is zero below lo_ds
                         // (and above hi_ds) too, since a query with one key has no gradient through its weight of one.
@@ -529,14 +541,14 @@ packed_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                             hi = end - j * BK - wg * 64;
                             hi_ds = end == 1 ? 0 : hi;
                         } else {
-                            const int t0 = (w.first + j) << (7 - g_shift);
-                            beyond = (w.len - t0) << g_shift;
+                            const int k_shift = prm.k_shift, t0 = (w.first + j) << (7 - k_shift);
+                            beyond = (w.len - t0) << k_shift;
                             masked = beyond < BK || w.len == 1;
                             hi = beyond - wg * 64;
                             if (prm.keys.causal) {
                                 masked |= t0 < w.tok0 + BM;
-                                lo = (tok - t0) * (1 << g_shift) - wg * 64;
-                                lo_ds = max(lo, (1 - t0) * (1 << g_shift) - wg * 64);
+                                lo = (tok - t0) * (1 << k_shift) - wg * 64;
+                                lo_ds = max(lo, (1 - t0) * (1 << k_shift) - wg * 64);
                             } else if (w.len == 1) {
                                 lo_ds = 64;
                             }
@@ -768,6 +780,48 @@ packed_delta_kernel(const __nv_bfloat16 *dout, const __nv_bfloat16 *out, const f
     }
 }
 
+// dk, dv of the sequences' rows from the parts' sums, in the parts' order: four columns a thread.
+template <int HD>
+__global__ void __launch_bounds__(256)
+packed_sum_kernel(const float *partial, const int *cu, int n_seq, __nv_bfloat16 *dk, __nv_bfloat16 *dv, int splits, int total, Divider kv_heads,
+                  long long dk_t, long long dk_h, long long dv_t, long long dv_h, float scale) {
+    const unsigned at = blockIdx.x * 256 + threadIdx.x, row = at / (HD / 4), c = at % (HD / 4) * 4, which = blockIdx.y;
+    const unsigned t = kv_heads.quotient(row), h = row - t * kv_heads.d;
+    allow_next();
+    wait_for_previous();
+    // rows between the first sequence's first and the last one's last belong to one of them
+    if ((int)t < max(cu[0], 0) || (int)t >= min(cu[n_seq], total)) return;
+    const long long size = (long long)total * kv_heads.d * HD;
+    const float *p = partial + which * size + (long long)row * HD + c;
+    float4 a = *reinterpret_cast<const float4 *>(p);
+    for (int i = 1; i < splits; ++i) {
+        const float4 b = *reinterpret_cast<const float4 *>(p + 2 * size * i);
+        a.x += b.x, a.y += b.y, a.z += b.z, a.w += b.w;
+    }
+    const float mul = which ? 1.f : scale;
+    __nv_bfloat16 *const to = which ? dv + t * dv_t + h * dv_h + c : dk + t * dk_t + h * dk_h + c;
+    *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(a.x * mul, a.y * mul), pack_bf16(a.z * mul, a.w * mul));
+}
+
+// Into how many parts DKV units take the group's heads.  Few key tiles with many heads would leave SMs idle while the longest
+// streams all heads' queries one after the other: a unit an SM is wanted, the smallest divisor of the group that gives it.  More
+// cost partial sums in memory and a launch to add them up; eight units an SM are the most, which bounds the sums to 155 MB where
+// the group's next divisor is a large one.  A sequence of one block gains nothing.  (4096 tokens, eight heads and one key head,
+// causal, us: one part 464, four 154, eight 121; eight prompts of 1 ... 511 tokens, three heads to a key head: one 41, three 35;
+// 2048 tokens, 32 heads over 8, causal, 153 in one part: 139 in two, 161 in four.)
+int key_splits(long long total, int n_seq, int heads, int kv_heads, int sms) {
+    const int group = heads / kv_heads;
+    if (total <= BM) return 1;
+    const long long units = (total / BM + std::min((long long)n_seq, total)) * kv_heads;
+    const long long most = std::min((long long)group, 8ll * sms / units);
+    int splits = 1;
+    for (int i = 2; i <= most && units * splits < sms; ++i)
+        if (group % i == 0) splits = i;
+    return splits;
+}
+
+constexpr size_t statistics_bytes(long long total, long long heads) { return (2 * (size_t)total * (size_t)heads * sizeof(float) + 255) / 256 * 256; }
+
 int opt_in(int device) {
     static std::mutex mutex;
     static bool done[64] = {};
@@ -798,7 +852,18 @@ int packed::backward_status(bool *expired) {
 using namespace hilberta;
 
 extern "C" size_t hilberta_packed_workspace(int total, int heads) {
-    return total > 0 && heads > 0 ? 2 * (size_t)total * (size_t)heads * sizeof(float) : 0;
+    if (total <= 0 || heads <= 0) return 0;
+    // statistics of every row; where key tiles are few, partial sums: the most that any number of key heads and sequences takes
+    const size_t stats = 2 * (size_t)total * (size_t)heads * sizeof(float);
+    int dev = -1;
+    const int sms = cudaGetDevice(&dev) == cudaSuccess ? sm100_count(dev) : 0;
+    size_t most = 0;
+    for (int kv = 1; kv <= heads && kv < sms; ++kv) {
+        if (heads % kv) continue;
+        const int splits = key_splits(total, 1, heads, kv, sms);
+        if (splits > 1) most = std::max(most, (size_t)splits * 2 * (size_t)total * (size_t)kv * 128 * sizeof(float));
+    }
+    return most ? statistics_bytes(total, heads) + most : stats;
 }
 
 extern "C" int hilberta_packed_backward(const void *dout, const void *q, const void *k, const void *v, const void *out, const float *lse,
@@ -846,11 +911,22 @@ extern "C" int hilberta_packed_backward(const void *dout, const void *q, const v
     int64_t bits = (int64_t)((uintptr_t)dq | (uintptr_t)dk | (uintptr_t)dv);
     for (int i = 10; i < 16; ++i) bits |= 2 * strides[i];
     p.align32 = (bits & 31) == 0;
-    CUtensorMap mq, mk, mv, mdo;
+    p.splits = key_splits(total, n_seq, heads, kv_heads, sms);
+    const int k_heads = p.group / p.splits, gk = packed::packed_heads(k_heads);
+    p.k_shift = __builtin_ctz((unsigned)gk);
+    p.k_odd = k_heads / gk;
+    p.partial = p.splits > 1 ? (float *)((char *)workspace + statistics_bytes(total, heads)) : nullptr;
+    CUtensorMap mq, mk, mv, mdo, mqs, mdos;
     if ((rc = packed::make_map(&mdo, dout, total, heads, head_dim, strides[0], strides[1], g, per_tile)) != HILBERTA_OK) return rc;
     if ((rc = packed::make_map(&mq, q, total, heads, head_dim, strides[2], strides[3], g, per_tile)) != HILBERTA_OK) return rc;
     if ((rc = packed::make_map(&mk, k, total, kv_heads, head_dim, strides[4], strides[5], 1, BM)) != HILBERTA_OK) return rc;
     if ((rc = packed::make_map(&mv, v, total, kv_heads, head_dim, strides[6], strides[7], 1, BM)) != HILBERTA_OK) return rc;
+    mqs = mq;
+    mdos = mdo;
+    if (gk != g) {
+        if ((rc = packed::make_map(&mdos, dout, total, heads, head_dim, strides[0], strides[1], gk, BM / gk)) != HILBERTA_OK) return rc;
+        if ((rc = packed::make_map(&mqs, q, total, heads, head_dim, strides[2], strides[3], gk, BM / gk)) != HILBERTA_OK) return rc;
+    }
     cudaStream_t st = (cudaStream_t)stream;
     const bool overlap = (size_t)total * heads * head_dim * 2 <= kOverlapBytes / 4;
     const int rows_per_block = 256 / (head_dim / 8) * 4;
@@ -861,10 +937,17 @@ extern "C" int hilberta_packed_backward(const void *dout, const void *q, const v
                                (long long)strides[1], (long long)strides[8], (long long)strides[9]));
     HB_LAUNCHED();
     auto units = [&](int per, int parts) { return (unsigned)(((long long)total / per + std::min(n_seq, total)) * parts); };   // at most
-    p.dkv_units = units(BM, kv_heads);
+    p.dkv_units = units(BM, kv_heads * p.splits);
     const unsigned ctas = p.dkv_units + units(per_tile, kv_heads * p.odd);
     HB_CUDA(launch_overlapping(head_dim == 128 ? packed_bwd_kernel<128> : packed_bwd_kernel<64>, ctas, THREADS, (size_t)SMEM_BYTES, 1, st,
-                               true, mq, mk, mv, mdo, p));
+                               true, mq, mk, mv, mdo, mqs, mdos, p));
     HB_LAUNCHED();
+    if (p.splits > 1) {
+        const long long vectors = (long long)total * kv_heads * (head_dim / 4);   // splits are few where this is large: below 2^31
+        HB_CUDA(launch_overlapping(head_dim == 128 ? packed_sum_kernel<128> : packed_sum_kernel<64>, dim3((unsigned)((vectors + 255) / 256), 2), 256, 0,
+                                   1, st, true, (const float *)p.partial, cu_seqlens, n_seq, p.dk, p.dv, p.splits, total, Divider(kv_heads), p.dk_t,
+                                   p.dk_h, p.dv_t, p.dv_h, p.scale));
+        HB_LAUNCHED();
+    }
     return HILBERTA_OK;
 }
