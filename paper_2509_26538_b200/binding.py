@@ -443,7 +443,7 @@ def _row_stride(t, name):
         if rows == 1:
             stride = st
         rows *= n
-    return max(stride, shape[-1])
+    return stride if rows > 1 else shape[-1]
 
 
 def _norm_weights(x, a, b):

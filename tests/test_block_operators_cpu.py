@@ -199,3 +199,12 @@ def test_slices_of_one_buffer_pass_the_overlap_test(lib):
     assert _packed(lib, q=base, k=far, v=far + (1 << 30), out=base + 128, kv=4, st=pairs) == hb.ERR_CUDA
     assert _packed(lib, q=base, k=far, v=far + (1 << 30), out=base + 112, kv=4, st=pairs) == hb.ERR_INVALID
     assert lib.hilberta_packed_workspace(10, 4) == 320 and lib.hilberta_packed_workspace(0, 4) == 0
+
+
+def test_row_stride_of_broadcast_and_overlapping_rows():
+    one, line = torch.zeros((1, 8)), torch.zeros(40)
+    assert hb._row_stride(one.expand(4, 8), "x") == 0 and hb._row_stride(one.expand(2, 3, 8), "x") == 0
+    assert hb._row_stride(line.as_strided((4, 8), (4, 1)), "x") == 4
+    assert hb._row_stride(line.as_strided((1, 8), (4, 1)), "x") == 8   # one row has any stride
+    with pytest.raises(ValueError):
+        hb._row_stride(torch.zeros((2, 1, 8)).expand(2, 3, 8), "x")

@@ -300,3 +300,18 @@ def test_refusals():
     assert n > 0
     hb.layer_norm(big, w, None, torch.empty_like(big), m, m.clone())
     hb.layer_norm_backward(big, big, w, m, m, None, torch.empty_like(w), None, workspace=torch.empty(n, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("cols", [64, 200, 1001, 1024])
+def test_broadcast_rows(cols, dtype):
+    x, dy, w = _make((37, cols), dtype, 40), _make((1, cols), dtype, 41), _make((cols,), dtype, 42)
+    y, mean, rstd = _check_forward(x[:1].expand(37, cols), w, None, y=torch.empty_like(x))
+    assert (y == y[0]).all()
+    _check_backward(x[:1].expand(37, cols), w, mean, rstd, dy.expand(37, cols), dx=torch.empty_like(x))
+    _, mean, rstd = _check_forward(x, w, None)
+    _check_backward(x, w, mean, rstd, dy.expand(37, cols), dx=torch.empty_like(x))
+    for out in (x[:1].expand(37, cols), torch.zeros(40 * cols, dtype=dtype, device="cuda").as_strided((37, cols), (cols // 2, 1))):
+        with pytest.raises(hb.HilbertaError) as e:
+            hb.layer_norm(y, w, None, out)
+        assert e.value.status == hb.ERR_INVALID
