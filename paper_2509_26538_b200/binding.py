@@ -423,6 +423,15 @@ def _scratch(n, like, stream):
         return like.new_empty(n, dtype=torch.uint8)
 
 
+def _zero(t, stream):
+    import torch
+    if stream is None:
+        t.zero_()
+    else:
+        with torch.cuda.stream(stream):
+            t.zero_()
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -534,6 +543,10 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, unit_offs
                                             _stream_ptr(stream))
     if status:
         _check(status, "hilberta_layer_norm_backward")
+    if not rows:   # how many groups there are without a row, the library cannot tell
+        for g in (dweight, dbias):
+            if g is not None and g.dim() == 2:
+                _zero(g, stream)
     return dx, dweight, dbias
 
 

@@ -315,3 +315,17 @@ def test_broadcast_rows(cols, dtype):
         with pytest.raises(hb.HilbertaError) as e:
             hb.layer_norm(y, w, None, out)
         assert e.value.status == hb.ERR_INVALID
+
+
+def test_no_rows_in_several_groups():
+    x, w, e = torch.empty((3, 0, 64), device="cuda"), torch.ones((3, 64), device="cuda"), torch.empty((3, 0), device="cuda")
+    both = torch.full((3, 128), 5.0, device="cuda")
+    hb.layer_norm_backward(x, x, w, e, e, None, both[:, :64], None)
+    assert (both[:, :64] == 0).all() and (both[:, 64:] == 5).all()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    hb.layer_norm_backward(x, x, w, e, e, None, both[:, :64], both[:, 64:], stream=side)
+    side.synchronize()
+    assert (both == 0).all()
+    none = torch.empty((0, 5, 64), device="cuda")
+    hb.layer_norm_backward(none, none, None, e, e, None, both[:0, :64], both[:0, 64:])
