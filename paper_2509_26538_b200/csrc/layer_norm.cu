@@ -410,6 +410,7 @@ layer_norm_bwd_kernel(const BackwardParams prm) {
             uint32_t bytes = mine ? (uint32_t)(((at + (size_t)cols * sizeof(T) + 15) & ~(uintptr_t)15) - from) : 0u;
             if (dense) bytes = r == 0 ? bytes * live : 0u;
             const uint32_t sum = __reduce_add_sync(0xffffffffu, bytes);
+            __syncwarp();   // all lanes' statistics come before lane 0's arrival
             if (lane == 0) ptx::mbar_expect_tx(full0 + 8 * s, sum);
             __syncwarp();
             if (bytes) bulk_load(ptx::smem_u32(ring) + (uint32_t)((s * 2 * rows + lane) * pitch), (const void *)from, bytes, full0 + 8 * s);
@@ -763,7 +764,6 @@ BackwardShape backward_shape(const Shape &s, bool aligned, int sms) {
     const int limit = (g.warps == MAX_WARPS ? 200 : 110) << 10;
     while (g.r > 1 && 3 * 2 * g.r * g.teams * g.pitch > limit) g.r /= 2;
     while (g.teams > 1 && 3 * 2 * g.r * g.teams * g.pitch > limit) --g.teams;
-    // few rows: on all SMs
     return g;
 }
 
