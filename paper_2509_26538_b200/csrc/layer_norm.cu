@@ -9,8 +9,9 @@
 // around the mean that has already been summed (no difference of large squares).
 // Measured (B200, us; share of the copy bandwidth).  Forward: 33792 x 1536 bf16, modulated 40 (79 %), 40000 x 1024 bf16 29 (85 %),
 // 12000 x 4096 fp32 64 (94 %): what is left in bf16 is unpacking and packing on the integer pipe, half busy.  Backward: 40000 x
-// 1024 bf16 48 (78 %), 36864 x 1152 bf16 56 (69 %), 12000 x 4096 fp32 107 (84 %), of which 5 ... 7 add the CTAs' sums up; rows that
-// are not aligned take elements one by one (30000 x 1001 bf16 forward 48, backward 62: 38 and 44 %).
+// 1024 bf16 46 (82 %), 36864 x 1152 bf16 54 (73 %), 12000 x 4096 fp32 97 (93 %), 3000 x 16000 bf16 97 (45 %: a row at a time, 15
+// warps and one barrier a row), of which 5 ... 7 add the CTAs' sums up; rows that are not aligned take elements one by one (30000 x
+// 1001 bf16 forward 48, backward 67: 38 and 41 %).
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -362,14 +363,14 @@ layer_norm_bwd_lanes_kernel(const BackwardParams prm) {
 // one behind: the granules are those of its own first and last elements.  Columns behind the row's end count as zeros.
 constexpr int MAX_STAGES = 4, MAX_ROWS = 16, MAX_WARPS = 16;
 template <class T, class W, int VEC, int NV, int R>
-__global__ void __launch_bounds__(32 * (MAX_WARPS + 1))
+__global__ void __launch_bounds__(NV * VEC <= 16 ? 32 * (MAX_WARPS + 1) : 32 * MAX_WARPS)
 layer_norm_bwd_kernel(const BackwardParams prm) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ __align__(16) float part[2][MAX_WARPS][2 * R];
     __shared__ __align__(16) float2 stats[MAX_STAGES][MAX_ROWS];   // -mean, rstd of a stage's rows
     __shared__ uint64_t full[MAX_STAGES], empty[MAX_STAGES];
     constexpr int P = NV * VEC / 2;           // pairs of a thread
-    constexpr bool KEEP_W = NV * VEC <= 16;   // weights in registers, else from the first-level cache
+    constexpr bool KEEP_W = NV * VEC <= 16;   // weights in registers, else behind the ring
     const int cols = prm.cols, all = (int)blockDim.x / 32 - 1, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int warps = prm.team_warps, teams = all / warps, rows = teams * R;   // rows of a round
     const int stages = prm.stages, pitch = prm.pitch;                          // pitch: bytes of a row in the ring
@@ -418,32 +419,40 @@ layer_norm_bwd_kernel(const BackwardParams prm) {
     }
     const int team = warp / warps, threads = 32 * warps, tid = (warp - team * warps) * 32 + lane;
     const W *weight = prm.weight ? (const W *)prm.weight + blockIdx.y * prm.stride_w : nullptr;
+    W *const kept = reinterpret_cast<W *>(ring + prm.stages * 2 * rows * pitch);
     const float inv_cols = 1.f / (float)cols;
     float2 dw[P] = {}, db[P] = {}, w[KEEP_W ? P : (VEC > 1 ? VEC / 2 : 1)];
-    // this thread's vector v: its column
-    auto col = [&](int v) { return (v * threads + tid) * VEC; };
+    // This thread's vector v: its column, and whether there is one.  A warp's vectors lie side by side, at distances that the
+    // compiler knows (up to 36 registers otherwise, whose spills come back from L2: 3000 x 10001 bf16 250 us, 83 so; 12000 x
+    // 4096 fp32 102 and 97; 30000 x 1001 bf16 79 and 67), but the team's where few vectors are of 8 bytes or single fp32 elements
+    // (36864 x 1152 bf16 79 us with a warp's side by side, 54 so; 3 x 1777 x 777 fp32 20 and 17.7).
+    constexpr bool NEAR = !KEEP_W || VEC * sizeof(T) >= 16 || VEC * sizeof(T) == 2;
+    const int apart = NEAR ? 32 * VEC : threads * VEC;
+    const int col0 = (NEAR ? tid / 32 * NV * 32 + lane : tid) * VEC, after = cols - col0;
+    auto col = [&](int v) { return col0 + v * apart; };
+    auto has = [&](int v) { return v * apart < after; };
     // pairs of vector v (VEC > 1) or of elements v and v + 1 (VEC = 1), zeros behind the row's end
     auto load_pairs = [&](float2 *to, const auto *row, int v) {
         using E = std::remove_cv_t<std::remove_pointer_t<decltype(row)>>;
         if constexpr (VEC > 1) {
             Vec<E, VEC> t;
             t.zero();
-            if (col(v) < cols) t.load(row + col(v));
+            if (has(v)) t.load(row + col(v));
 #pragma unroll
             for (int e = 0; e < VEC / 2; ++e) to[e] = t.pair(e);
         } else {
             Vec<E, 1> t0, t1;
             t0.zero();
             t1.zero();
-            if (col(v) < cols) t0.load(row + col(v));
-            if (col(v + 1) < cols) t1.load(row + col(v + 1));
+            if (has(v)) t0.load(row + col(v));
+            if (has(v + 1)) t1.load(row + col(v + 1));
             to[0] = make_float2(t0.get(0), t1.get(0));
         }
     };
     constexpr int STEP = VEC > 1 ? 1 : 2, PV = VEC > 1 ? VEC / 2 : 1;   // vectors and pairs at a time
     auto load_w = [&](float2 *to, int v) {
         if (weight) {
-            load_pairs(to, weight, v);
+            load_pairs(to, KEEP_W ? weight : (const W *)kept, v);
 #pragma unroll
             for (int e = 0; e < PV; ++e) to[e] = __fadd2_rn(to[e], both(prm.offset));
         } else {
@@ -454,6 +463,13 @@ layer_norm_bwd_kernel(const BackwardParams prm) {
     if (warp < all && KEEP_W) {
 #pragma unroll
         for (int v = 0; v < NV; v += STEP) load_w(w + v / STEP * PV, v);
+    }
+    if (warp < all && !KEEP_W && weight) {   // a thread's own columns, for itself
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            Vec<W, VEC> t;
+            if (has(v)) t.load(weight + col(v)), t.store(kept + col(v));
+        }
     }
     // VEC = 1: where a row starts within its granule
     const T *x0 = (const T *)prm.x + (first + team * R) * prm.stride_x, *dy0 = (const T *)prm.dy + (first + team * R) * prm.stride_dy;
@@ -552,8 +568,8 @@ layer_norm_bwd_kernel(const BackwardParams prm) {
                     }
                     Vec<T, VEC> o;
                     o.set(f);
-                    if (col(v) < cols) o.store(out + col(v));
-                    if (VEC == 1 && col(v + 1) < cols) {
+                    if (has(v)) o.store(out + col(v));
+                    if (VEC == 1 && has(v + 1)) {
                         o.set(f + 1);
                         o.store(out + col(v + 1));
                     }
@@ -729,7 +745,7 @@ struct BackwardShape {
     long long round() const { return lanes ? (long long)r * (256 / lanes) : (long long)r * teams; }   // rows of a round
 };
 
-BackwardShape backward_shape(const Shape &s, bool aligned, int sms) {
+BackwardShape backward_shape(const Shape &s, bool aligned) {
     BackwardShape g{};
     if (s.cols <= 256 && (aligned || s.cols <= 32)) {
         g.lanes = s.cols <= 8 * 8 && aligned ? 8 : 32;
@@ -737,11 +753,13 @@ BackwardShape backward_shape(const Shape &s, bool aligned, int sms) {
         return g;
     }
     // Columns of a thread: with 16-byte vectors multiples of 8 (4 in fp32), with 8-byte ones of 4.  The fewest idle slots,
-    // then the fewest columns, 8 at least.
+    // then the fewest columns, 8 at least.  More than 16 take 128 registers a thread, which 16 warps with the one that fills the
+    // ring can have (17 have 96).
     long long best = -1;
     const int full = aligned ? (int)(16 / s.esz) : 1;
-    const int most = s.cols > MAX_WARPS * 32 * 16 ? 32 : 16;
-    for (int warps = MAX_WARPS; warps >= 1; --warps)
+    const bool wide = s.cols > MAX_WARPS * 32 * 16;
+    const int most = wide ? 36 : 16;
+    for (int warps = wide ? MAX_WARPS - 1 : MAX_WARPS; warps >= 1; --warps)
         for (int vec = full; vec >= std::min(full, 4); vec /= 2) {
             const int unit = std::max(vec, 4), each = (s.cols + 32 * warps * unit - 1) / (32 * warps * unit) * unit;
             if (each > most || (each < 8 && s.cols >= 8 * 32)) continue;
@@ -761,7 +779,7 @@ BackwardShape backward_shape(const Shape &s, bool aligned, int sms) {
     g.teams = g.warps & (g.warps - 1) ? 1 : std::max(1, std::min((aligned ? 8 : 16) / g.warps, MAX_ROWS / g.r));
     // Three rounds of the ring in half of an SM, in all of it for a CTA that fills the SM anyway (12000 x 4096 fp32, us: 2 CTAs of
     // one row at a time 118, 1 CTA of two rows 98).
-    const int limit = (g.warps == MAX_WARPS ? 200 : 110) << 10;
+    const int limit = (wide || g.warps == MAX_WARPS ? 200 : 110) << 10;
     while (g.r > 1 && 3 * 2 * g.r * g.teams * g.pitch > limit) g.r /= 2;
     while (g.teams > 1 && 3 * 2 * g.r * g.teams * g.pitch > limit) --g.teams;
     return g;
@@ -805,14 +823,15 @@ int launch_backward(BackwardCall &c) {
     const int threads = 32 * (g.warps * g.teams + 1), stage = 2 * g.r * g.teams * g.pitch;
     // rows, and afterwards the sums of a team: NV VEC columns, dw and db, of each of its threads
     const int least = g.teams > 1 ? NV * VEC * 8 * 32 * g.warps : 0;
-    auto ring = [&](int stages) { return std::max(stages * stage, least); };
+    const int kept = NV * VEC > 16 && c.prm.weight ? g.pitch / (int)sizeof(T) * (int)sizeof(W) : 0;   // weights behind the ring
+    auto ring = [&](int stages) { return std::max(stages * stage + kept, least); };
     // As many CTAs as run at once with three rounds each (the driver's count, asked once for each shape in turn), then
     // more rounds if that costs none.
     static std::atomic<uint64_t> asked{0};   // threads, stage, stages and CTAs of the last answer
-    const uint64_t key = (uint64_t)threads << 40 | (uint64_t)stage << 8;
+    const uint64_t key = (uint64_t)threads << 40 | (uint64_t)stage << 8 | (kept ? 1ull << 63 : 0);
     uint64_t known = asked.load();
     if ((known & ~0xffull) != key) {
-        int stages = std::min(3, std::max(1, (220 << 10) / stage)), per_sm = 0, more = 0;
+        int stages = std::min(3, std::max(1, ((220 << 10) - kept) / stage)), per_sm = 0, more = 0;
         HB_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, (size_t)ring(stages)));
         if (stages == 3 && ring(4) <= 220 << 10) {
             HB_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&more, kernel, threads, (size_t)ring(4)));
@@ -864,6 +883,7 @@ int backward_by_each(BackwardCall &c) {
             case 12: return backward_by_rows<T, W, VEC, 12>(c);
             case 20: return backward_by_rows<T, W, VEC, 20>(c);
             case 28: return backward_by_rows<T, W, VEC, 28>(c);
+            case 36: return backward_by_rows<T, W, VEC, 36>(c);
         }
     }
     return HILBERTA_ERR_UNSUPPORTED;
@@ -924,7 +944,7 @@ extern "C" size_t hilberta_layer_norm_workspace(int64_t rows, int cols, int64_t 
     for (size_t esz : {2, 4})   // whatever the type and the alignment
         for (bool aligned : {false, true}) {
             s.esz = esz;
-            const BackwardShape g = backward_shape(s, aligned, sms);
+            const BackwardShape g = backward_shape(s, aligned);
             ctas = std::max(ctas, std::min((s.rows_per_group + g.round() - 1) / g.round(), (long long)sms * MAX_PER_SM / std::max(1ll, s.groups)));
         }
     return ctas > 1 ? (size_t)(ctas * s.groups) * 2 * (size_t)cols * sizeof(float) : 0;
@@ -967,7 +987,7 @@ extern "C" int hilberta_layer_norm_backward(const void *dy, const void *x, const
                          aligned16(weight, prm.stride_w, s.wsz) && aligned16(dweight, prm.stride_dw, s.wsz) &&
                          aligned16(dbias, prm.stride_dw, s.wsz);
     BackwardCall c{};
-    c.g = backward_shape(s, vectors, sms);
+    c.g = backward_shape(s, vectors);
     prm.team_warps = c.g.warps;
     prm.pitch = c.g.pitch;
     c.prm = prm;

@@ -329,3 +329,24 @@ def test_no_rows_in_several_groups():
     assert (both == 0).all()
     none = torch.empty((0, 5, 64), device="cuda")
     hb.layer_norm_backward(none, none, None, e, e, None, both[:0, :64], both[:0, 64:])
+
+
+@pytest.mark.parametrize("dtype,wdtype", [(torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float32, torch.float32)])
+@pytest.mark.parametrize("cols", [8193, 8200, 8320, 10001, 10240, 11000, 12284, 12288, 14000, 15001, 16000, 16376])
+def test_wide_rows(cols, dtype, wdtype):
+    for rows in (1, 4, 331):
+        x, w = _make((rows, cols), dtype, cols + rows), _make((cols,), wdtype, 1, 1.0, 0.3)
+        _, mean, rstd = _check_forward(x, w, None)
+        dy = _make((rows, cols), dtype, 3, 0.1, 1.0)
+        _check_backward(x, w, mean, rstd, dy)
+        _check_backward(x, None, mean, rstd, dy, wlike=w)
+
+
+def test_wide_rows_in_groups_and_slices():
+    cols = 9000
+    x, mod = _make((3, 40, cols), torch.bfloat16, 50), _make((3, 2 * cols), torch.bfloat16, 51, 0.0, 0.3)
+    _, mean, rstd = _check_forward(x, mod[:, :cols], mod[:, cols:], unit=True)
+    _check_backward(x, mod[:, :cols], mean, rstd, _make((3, 40, cols), torch.bfloat16, 52), unit=True)
+    big = _make((40, 2 * cols + 3), torch.bfloat16, 53)
+    _, mean, rstd = _check_forward(big[:, 3:3 + cols], mod[0, :cols], None, y=torch.empty((40, cols), dtype=torch.bfloat16, device="cuda"))
+    _check_backward(big[:, 3:3 + cols], mod[0, :cols], mean, rstd, big[:, cols:2 * cols], dx=torch.empty((40, cols), dtype=torch.bfloat16, device="cuda"))
