@@ -655,6 +655,8 @@ using namespace hilberta;
 
 extern "C" int hilberta_packed_status(void) {
     bool expired = false;
+    // kernels on every stream: the copies below wait for none on a non-blocking one
+    HB_CUDA(cudaDeviceSynchronize());
     int rc = packed::forward_status(&expired);
     if (rc == HILBERTA_OK) rc = packed::backward_status(&expired);
     return rc != HILBERTA_OK ? rc : expired ? HILBERTA_ERR_TIMEOUT : HILBERTA_OK;
