@@ -416,7 +416,11 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 const bool top_on_fma = mx_fma > mx_mufu;
                 const float mx = mx_raw * scale_log2;
                 if (j == 0) {
-                    m_ref = mx;
+                    // A row behind the sequence has no vote on the warp's references, which would change the roundings of the
+                    // others with what a neighbour's query happens to be: nothing exceeds its own.  (A register for the
+                    // threshold instead costs 1 %.)
+                    const Work w = work();
+                    m_ref = w.tok0 + ((t * BM + r) >> prm.g_shift) < w.len ? mx : __int_as_float(0x7f800000);
                 } else if (__any_sync(0xffffffffu, mx > m_ref + RESCALE_THRESHOLD)) {
                     // the accumulator of the blocks so far belongs to the old reference
                     ok = wait_or_abort(bar(PV_DONE + t), (cPV - 1) & 1, &abort_flag, status, 0x303 + t);
