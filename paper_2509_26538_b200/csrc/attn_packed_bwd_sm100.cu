@@ -80,6 +80,7 @@ struct Params {
     long long dq_t, dq_h, dk_t, dk_h, dv_t, dv_h;
     float scale, scale_log2;
     int align32;
+    long long unit_wait;   // of waits that last a whole unit
 };
 
 // What every role derives from a unit.
@@ -203,7 +204,7 @@ packed_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     uint32_t uc = 0;
     auto next_unit = [&](packed::Unit &u, bool release, int code) {
         const uint32_t s = uc % UNITS;
-        if (!wait_or_abort(bar(U_FULL + s), (uc / UNITS) & 1, abort_flag, status, code)) return false;
+        if (!wait_or_abort(bar(U_FULL + s), (uc / UNITS) & 1, abort_flag, status, code, prm.unit_wait)) return false;
         u = units[s];
         ++uc;
         if (release) mbar_arrive(bar(U_EMPTY + s));
@@ -331,12 +332,12 @@ packed_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             if (!found) u.len = -1;
             if (lane == 0) {
                 const uint32_t s = i % UNITS;
-                ok = wait_or_abort(bar(U_EMPTY + s), ((i / UNITS) & 1) ^ 1, abort_flag, status, 0x406);
+                ok = wait_or_abort(bar(U_EMPTY + s), ((i / UNITS) & 1) ^ 1, abort_flag, status, 0x406, prm.unit_wait);
                 if (ok) {
                     units[s] = u;
                     mbar_arrive(bar(U_FULL + s));
                     // free once the last R T^T MMA of the previous unit has retired
-                    if (found && i > 0) ok = wait_or_abort(bar(RES_EMPTY), (i - 1) & 1, abort_flag, status, 0x401);
+                    if (found && i > 0) ok = wait_or_abort(bar(RES_EMPTY), (i - 1) & 1, abort_flag, status, 0x401, prm.unit_wait);
                     if (found && ok) {
                         const bool dkv = u.mode == MODE_DKV;
                         const Work w = dkv ? work_of<MODE_DKV>(prm, u) : work_of<MODE_DQ>(prm, u);
@@ -348,7 +349,7 @@ packed_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                             tma_load_4d(sR2 + sl * SLAB_BYTES, dkv ? &tmV : &tmdO, bar(RES_FULL), 64 * sl, head, w.row0 + w.tok0, 0);
                         }
                         // not before the producer is through with this unit: one that another CTA could start sooner is left to it
-                        ok = wait_or_abort(bar(WANT), i & 1, abort_flag, status, 0x408);
+                        ok = wait_or_abort(bar(WANT), i & 1, abort_flag, status, 0x408, prm.unit_wait);
                     }
                 }
             }
@@ -373,7 +374,7 @@ packed_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             __syncwarp();
             if (!ok) break;
             if (lane == 0) mbar_arrive(bar(U_EMPTY + (uc - 1) % UNITS));
-            ok = wait_or_abort(bar(OUT_FULL), n & 1, abort_flag, status, 0x607);
+            ok = wait_or_abort(bar(OUT_FULL), n & 1, abort_flag, status, 0x607, prm.unit_wait);
             if (!ok) break;
             tc_fence_after();
             auto store = [&](auto mode) {
@@ -915,6 +916,8 @@ extern "C" int hilberta_packed_backward(const void *dout, const void *q, const v
     const int k_heads = p.group / p.splits, gk = packed::packed_heads(k_heads);
     p.k_shift = __builtin_ctz((unsigned)gk);
     p.k_odd = k_heads / gk;
+    // blocks of the longest unit there may be: keys of a query tile, or queries of the heads of a key tile
+    p.unit_wait = packed::unit_wait((((long long)total << p.k_shift) + BK - 1) / BK * p.k_odd);
     p.partial = p.splits > 1 ? (float *)((char *)workspace + statistics_bytes(total, heads)) : nullptr;
     CUtensorMap mq, mk, mv, mdo, mqs, mdos;
     if ((rc = packed::make_map(&mdo, dout, total, heads, head_dim, strides[0], strides[1], g, per_tile)) != HILBERTA_OK) return rc;

@@ -68,6 +68,7 @@ struct Params {
     __nv_bfloat16 *out;
     float *lse;
     float scale_log2;
+    long long unit_wait;              // of waits that last a whole unit
 };
 
 // What every role derives from a unit.
@@ -181,7 +182,7 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     uint32_t uc = 0;
     auto next_unit = [&](packed::Unit &u, int code) {
         const uint32_t s = uc % UNITS, ph = (uc / UNITS) & 1;
-        if (!wait_or_abort(bar(U_FULL + s), ph, &abort_flag, status, code)) return false;
+        if (!wait_or_abort(bar(U_FULL + s), ph, &abort_flag, status, code, prm.unit_wait)) return false;
         u = units[s];
         ++uc;
         mbar_arrive(bar(U_EMPTY + s));
@@ -209,7 +210,7 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             if (!found) u.len = -1;
             const uint32_t s = i % UNITS, ph = (i / UNITS) & 1;
             if (lane == 0) {
-                ok = wait_or_abort(bar(U_EMPTY + s), ph ^ 1, &abort_flag, status, 0x108);
+                ok = wait_or_abort(bar(U_EMPTY + s), ph ^ 1, &abort_flag, status, 0x108, prm.unit_wait);
                 if (ok) {
                     units[s] = u;
                     mbar_arrive(bar(U_FULL + s));
@@ -218,7 +219,7 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
             if (!found || !ok) break;
             // not before the producer is through with this unit: a unit that another CTA could start sooner is left to it
-            if (lane == 0) ok = wait_or_abort(bar(WANT), i & 1, &abort_flag, status, 0x10a);
+            if (lane == 0) ok = wait_or_abort(bar(WANT), i & 1, &abort_flag, status, 0x10a, prm.unit_wait);
             ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0 && ask_next(n, more, asked);
         }
     } else if (warp == 8) {
@@ -341,7 +342,7 @@ packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         while (ok) {
             // The unit stays in its slot to the end, so that little of it lives in registers beside the scores.
             const uint32_t slot = uc % UNITS;
-            ok = wait_or_abort(bar(U_FULL + slot), (uc / UNITS) & 1, &abort_flag, status, 0x300);
+            ok = wait_or_abort(bar(U_FULL + slot), (uc / UNITS) & 1, &abort_flag, status, 0x300, prm.unit_wait);
             ++uc;
             const volatile packed::Unit &u = units[slot];
             if (!ok || u.len < 0) break;
@@ -703,6 +704,7 @@ extern "C" int hilberta_packed_forward(const void *q, const void *k, const void 
     p.lse = lse;
     const float s = scale > 0.f ? scale : 1.f / sqrtf((float)head_dim);
     p.scale_log2 = s * 1.4426950408889634f;
+    p.unit_wait = packed::unit_wait(((long long)total + BN - 1) / BN);
     CUtensorMap mq, mk, mv, mo;
     if ((rc = packed::make_map(&mq, q, total, heads, head_dim, strides[0], strides[1], g, per_tile)) != HILBERTA_OK) return rc;
     if ((rc = packed::make_map(&mk, k, total, kv_heads, head_dim, strides[2], strides[3], 1, BN)) != HILBERTA_OK) return rc;

@@ -20,7 +20,7 @@
 namespace hilberta {
 namespace packed {
 
-// Limit of `total`: a unit over so many keys still ends well within the bounded waits.
+// Limit of `total`: rows of a streamed block's coordinates, 16 heads to a token, stay well below 2^31.
 constexpr int MAX_TOTAL = 1 << 26;
 constexpr int MAX_SEQ = 65536;
 
@@ -146,6 +146,11 @@ bool overlap(const void *a, const int64_t *sa, int ha, const void *b, const int6
 // Codes of waits that gave up, of the forward and the backward kernels: read and cleared.
 int forward_status(bool *expired);
 int backward_status(bool *expired);
+
+// Deadline of waits that last a whole unit -- for the next unit, or for the end of this one in a role with little to do -- where the
+// others last a block.  A unit of up to `blocks` streamed blocks takes some 4000 cycles for each: four times that, behind the
+// usual second.  (64 heads to a key head and 2^20 tokens: 524288 blocks in a unit, more than a second.)
+inline long long unit_wait(long long blocks) { return ptx::WAIT_CYCLES + 16384 * blocks; }
 
 // The largest power of two that divides the heads of a group, at most 16: so many heads of one token are rows of a
 // query tile next to one another.
