@@ -381,6 +381,10 @@ int hilberta_layer_norm_backward(const void *dy, const void *x, const void *weig
                                  int64_t stride_w, int64_t stride_dw, int dtype, int weight_dtype, int unit_offset, void *stream);
 size_t hilberta_layer_norm_workspace(int64_t rows, int cols, int64_t rows_per_group);
 
+/* 0, or ERR_TIMEOUT if a bounded wait inside a backward kernel of the layer norm on the current device has given up
+ * since the last call (that call's gradients are undefined).  Synchronises the device.  Clears the flag. */
+int hilberta_layer_norm_status(void);
+
 /* Rotary positions, the step between the QKV projection and Algorithm 1 (Sec. 3.3 anchors them in the shared
  * region).  Pair j of every head turns by t = position[axis[j]] * inv_freq[j]:
  *     a' = factor * (a cos t - b sin t),   b' = factor * (a sin t + b cos t),
@@ -542,6 +546,9 @@ int hilberta_check_overlap(uint64_t a, uint64_t b, int batch, int heads, int S, 
  * return HILBERTA_ERR_TIMEOUT once and the device must stay usable.  Asynchronous on
  * `stream`. */
 int hilberta_selftest_timeout(hilberta_plan_t *plan, void *stream);
+
+/* The same for the layer norm's waits: after it, hilberta_layer_norm_status() must return HILBERTA_ERR_TIMEOUT once. */
+int hilberta_selftest_layer_norm_timeout(void *stream);
 
 /* Number of kernels the library has launched in this process (all entry points). */
 uint64_t hilberta_launch_count(void);

@@ -31,12 +31,12 @@ SYMBOLS = (
     "hilberta_backward_static", "hilberta_permute",
     "hilberta_unpermute",
     "hilberta_forward_host",
-    "hilberta_layer_norm", "hilberta_layer_norm_backward", "hilberta_layer_norm_workspace",
+    "hilberta_layer_norm", "hilberta_layer_norm_backward", "hilberta_layer_norm_workspace", "hilberta_layer_norm_status",
     "hilberta_rotary", "hilberta_rotary_backward", "hilberta_rotary_frequencies",
     "hilberta_packed_forward", "hilberta_packed_backward", "hilberta_packed_workspace", "hilberta_packed_status",
     "hilberta_check_work_list", "hilberta_check_overlap", "hilberta_schedule_units", "hilberta_cut_schedule",
     "hilberta_check_shares",
-    "hilberta_plan_status", "hilberta_selftest_timeout", "hilberta_launch_count", "hilberta_status_string", "hilberta_version",
+    "hilberta_plan_status", "hilberta_selftest_timeout", "hilberta_selftest_layer_norm_timeout", "hilberta_launch_count", "hilberta_status_string", "hilberta_version",
     "hilberta_last_cuda_error",
 )
 
@@ -103,6 +103,10 @@ def lib():
     L.hilberta_layer_norm_backward.restype = i32
     L.hilberta_layer_norm_workspace.argtypes = [i64, i32, i64]
     L.hilberta_layer_norm_workspace.restype = sz
+    L.hilberta_layer_norm_status.argtypes = []
+    L.hilberta_layer_norm_status.restype = i32
+    L.hilberta_selftest_layer_norm_timeout.argtypes = [vp]
+    L.hilberta_selftest_layer_norm_timeout.restype = i32
     f64 = ctypes.c_double
     for name in ("hilberta_rotary", "hilberta_rotary_backward"):
         f = getattr(L, name)
@@ -548,6 +552,11 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, unit_offs
             if g is not None and g.dim() == 2:
                 _zero(g, stream)
     return dx, dweight, dbias
+
+
+def layer_norm_status() -> int:
+    """0, or ERR_TIMEOUT if a wait inside a backward kernel of the layer norm has given up since the last call; synchronises."""
+    return int(lib().hilberta_layer_norm_status())
 
 
 def rotary_frequencies(pairs, base=10000.0, scaling=ROTARY_PLAIN, scale=1.0, context=0.0, slow=1.0, fast=32.0):

@@ -26,6 +26,8 @@ namespace {
 
 constexpr int MAX_COLS = 16384;
 
+__device__ int g_status[64];   // [0]: code of the first wait that gave up
+
 // VEC elements at p, as floats: one 16-byte load (VEC * sizeof(T) = 16, or 32 in two), or one element.
 template <class T, int VEC>
 struct Vec {
@@ -268,6 +270,21 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
                  : "memory");
 }
 
+// The ring's bounded wait.  One that gives up leaves its code in the status, and the CTA's other waits give up soon after it.
+// TRIES: it counts tries and has no clock, whose registers cost the kernel of two 16-byte bf16 vectors a thread and one row at a
+// time 7 ... 9 % (5120 and 6656 columns; 1 % so); the others are up to 10 % faster with the clock (10000 ... 14000 columns).
+template <bool TRIES>
+__device__ __forceinline__ bool ring_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, int code) {
+    if constexpr (!TRIES) return ptx::wait_or_abort(bar, parity, abort_flag, g_status, code);
+    if (ptx::mbar_try_wait(bar, parity)) return true;
+#pragma unroll 1
+    for (int i = 0; *abort_flag == 0 && i < (1 << 22); ++i)
+        if (ptx::mbar_try_wait(bar, parity)) return true;
+    *abort_flag = 1;
+    atomicCAS(g_status, 0, code);
+    return false;
+}
+
 // Sums over columns need every element of a row, sums over rows one column of all: a thread keeps its columns for all
 // rows that its CTA sees (2 NV VEC fp32 sums in registers), and the two sums of a row cross the team that shares the row.
 
@@ -369,7 +386,9 @@ layer_norm_bwd_kernel(const BackwardParams prm) {
     __shared__ __align__(16) float part[2][MAX_WARPS][2 * R];
     __shared__ __align__(16) float2 stats[MAX_STAGES][MAX_ROWS];   // -mean, rstd of a stage's rows
     __shared__ uint64_t full[MAX_STAGES], empty[MAX_STAGES];
+    __shared__ int abort_flag;
     constexpr int P = NV * VEC / 2;           // pairs of a thread
+    constexpr bool TRIES = VEC == 8 && NV == 2 && R == 1;
     constexpr bool KEEP_W = NV * VEC <= 16;   // weights in registers, else behind the ring
     const int cols = prm.cols, all = (int)blockDim.x / 32 - 1, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int warps = prm.team_warps, teams = all / warps, rows = teams * R;   // rows of a round
@@ -380,6 +399,7 @@ layer_norm_bwd_kernel(const BackwardParams prm) {
     const int rounds = first < row_end ? (int)((row_end - first + step - 1) / step) : 0;
     const uint32_t full0 = ptx::smem_u32(full), empty0 = ptx::smem_u32(empty);
     if (threadIdx.x == 0) {
+        abort_flag = 0;
         for (int i = 0; i < stages; ++i) {
             ptx::mbar_init(full0 + 8 * i, 1);
             ptx::mbar_init(empty0 + 8 * i, all);
@@ -404,8 +424,7 @@ layer_norm_bwd_kernel(const BackwardParams prm) {
             const int live = (int)min((long long)rows, row_end - r0);
             const bool mine = r < live;
             const float value = mine ? (of_x ? prm.mean : prm.rstd)[r0 + r] : 0.f;
-            // bounded, like every wait; the readers' arrivals cannot fail
-            ptx::mbar_wait(empty0 + 8 * s, ((i / stages) & 1) ^ 1);
+            if (!__all_sync(0xffffffffu, ring_wait<TRIES>(empty0 + 8 * s, ((i / stages) & 1) ^ 1, &abort_flag, 0x700))) break;
             if (r < rows) (of_x ? stats[s][r].x : stats[s][r].y) = of_x ? -value : value;
             const uintptr_t at = (uintptr_t)src, from = at & ~(uintptr_t)15;
             uint32_t bytes = mine ? (uint32_t)(((at + (size_t)cols * sizeof(T) + 15) & ~(uintptr_t)15) - from) : 0u;
@@ -482,7 +501,8 @@ layer_norm_bwd_kernel(const BackwardParams prm) {
         const uint8_t *const base = mine + s * 2 * to_dy;
         auto row_x = [&](int r) { return (const T *)(base + r * pitch + (VEC == 1 ? (int)((uintptr_t)(x0 + r * prm.stride_x) & 15) : 0)); };
         auto row_dy = [&](int r) { return (const T *)(base + to_dy + r * pitch + (VEC == 1 ? (int)((uintptr_t)(dy0 + r * prm.stride_dy) & 15) : 0)); };
-        ptx::mbar_wait(full0 + 8 * s, phase);
+        // a warp whose wait gives up goes on, through the barriers that the team's other warps are at; its next ones give up soon
+        ring_wait<TRIES>(full0 + 8 * s, phase, &abort_flag, 0x701);
         float2 st[R];
         float sum[2 * R];
 #pragma unroll
@@ -582,6 +602,12 @@ layer_norm_bwd_kernel(const BackwardParams prm) {
         if (++s == stages) s = 0, phase ^= 1;
         x0 += step * prm.stride_x;
         dy0 += step * prm.stride_dy;
+    }
+    if (*(volatile int *)&abort_flag) {
+        // let every copy already issued land before the CTA retires
+        const long long t0 = clock64();
+        while (clock64() - t0 < 2000000) {
+        }
     }
     if (!prm.dweight && !prm.dbias) return;
     // the teams' sums one after the other through the ring, team 0 first: the order is always the same
@@ -737,6 +763,19 @@ int forward_by_cols(const ForwardParams &prm, bool overlap, cudaStream_t stream)
 }
 
 constexpr int MAX_PER_SM = 8;   // CTAs of the backward kernels on one SM
+
+// One warp waits, with a deadline of 2 million cycles, on a barrier that nothing arrives on.
+__global__ void layer_norm_timeout_probe() {
+    __shared__ uint64_t never;
+    __shared__ int abort_flag;
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        ptx::mbar_init(ptx::smem_u32(&never), 1);
+        ptx::mbar_fence_init();
+    }
+    __syncthreads();
+    ptx::wait_or_abort(ptx::smem_u32(&never), 0, &abort_flag, g_status, 0x7e57, 2000000ll);
+}
 
 // How the backward pass is cut up.  lanes > 0: that many lanes have a row; else teams of `warps` warps, `each` columns a
 // thread and r rows at a time.
@@ -1012,4 +1051,24 @@ extern "C" int hilberta_layer_norm_backward(const void *dy, const void *x, const
         HB_LAUNCHED();
         return HILBERTA_OK;
     });
+}
+
+extern "C" int hilberta_layer_norm_status(void) {
+    int code = 0;
+    HB_CUDA(cudaDeviceSynchronize());
+    HB_CUDA(cudaMemcpyFromSymbol(&code, g_status, sizeof(int)));
+    if (!code) return HILBERTA_OK;
+    const int zero[3] = {0, 0, 0};
+    HB_CUDA(cudaMemcpyToSymbol(g_status, zero, sizeof(zero)));
+    return HILBERTA_ERR_TIMEOUT;
+}
+
+extern "C" int hilberta_selftest_layer_norm_timeout(void *stream) {
+    int dev = -1;
+    HB_CUDA(cudaGetDevice(&dev));
+    if (!sm100_count(dev)) return HILBERTA_ERR_ARCH;
+    layer_norm_timeout_probe<<<1, 32, 0, (cudaStream_t)stream>>>();
+    HB_CUDA(cudaGetLastError());
+    HB_LAUNCHED();
+    return HILBERTA_OK;
 }
