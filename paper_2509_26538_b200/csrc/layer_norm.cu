@@ -677,14 +677,6 @@ layer_norm_sums_kernel(const float *partial, void *dweight, void *dbias, int col
     }
 }
 
-// The rows x cols elements at a (row stride sa) and at b: apart, or the very same rows?
-bool rows_overlap(const void *a, long long sa, const void *b, long long sb, long long rows, int cols, size_t esz) {
-    if (!a || !b || (a == b && sa == sb)) return false;
-    const char *a0 = (const char *)a, *b0 = (const char *)b;
-    const long long la = ((rows - 1) * sa + cols) * (long long)esz, lb = ((rows - 1) * sb + cols) * (long long)esz;
-    return a0 < b0 + lb && b0 < a0 + la;
-}
-
 // Do `rows` rows of cols elements, stride apart, share a byte with as many at b?  (Two slices of one tensor may lie side by side.)
 bool slices_overlap(const void *a, const void *b, long long stride, long long rows, int cols, size_t esz) {
     if (!a || !b || rows < 1) return false;
@@ -693,6 +685,16 @@ bool slices_overlap(const void *a, const void *b, long long stride, long long ro
     if (rows == 1 || step == 0) return d < row;
     if (d >= (uintptr_t)(rows - 1) * step + row) return false;
     return d % step < row || d % step + row > step;
+}
+
+// The rows x cols elements at a (row stride sa) and at b: apart, or the very same rows?  Slices of one buffer (equal strides) may
+// lie side by side; the address ranges of others have to be apart.
+bool rows_overlap(const void *a, long long sa, const void *b, long long sb, long long rows, int cols, size_t esz) {
+    if (!a || !b || rows < 1) return false;
+    if (sa == sb || rows == 1) return a != b && slices_overlap(a, b, sa, rows, cols, esz);
+    const char *a0 = (const char *)a, *b0 = (const char *)b;
+    const long long la = ((rows - 1) * sa + cols) * (long long)esz, lb = ((rows - 1) * sb + cols) * (long long)esz;
+    return a0 < b0 + lb && b0 < a0 + la;
 }
 
 struct Shape {
