@@ -459,6 +459,11 @@ def _row_stride(t, name):
     return stride if rows > 1 else shape[-1]
 
 
+def _same_rows(a, b):
+    """Do two tensors of one shape lie alike?  An axis of one element has any stride."""
+    return all(n == 1 or i == j for n, i, j in zip(a.shape, a.stride(), b.stride()))
+
+
 def _norm_weights(x, a, b):
     """(rows per group, row stride, dtype code) of weight and bias, or of their gradients: [cols] or [groups, cols]."""
     w = b if a is None else a
@@ -466,7 +471,7 @@ def _norm_weights(x, a, b):
         return 0, 0, _dtype_code(x)
     shape, stride, xshape = w.shape, w.stride(), x.shape
     cols = xshape[-1]
-    if a is not None and b is not None and (b.shape != shape or b.dtype != w.dtype or b.stride() != stride):
+    if a is not None and b is not None and (b.shape != shape or b.dtype != w.dtype or (b.stride() != stride and not _same_rows(a, b))):
         raise ValueError("weight and bias (and their gradients): one shape, dtype and row stride")
     if shape[-1] != cols or (stride[-1] != 1 and cols > 1):
         raise ValueError("weights are [cols] or [groups, cols], the last axis contiguous")
