@@ -427,6 +427,13 @@ def _scratch(n, like, stream):
         return like.new_empty(n, dtype=torch.uint8)
 
 
+def _given(workspace):
+    """Bytes of a workspace that the caller brings: the library takes them as one run."""
+    if not workspace.is_contiguous():
+        raise ValueError("workspace: contiguous")
+    return workspace.nbytes
+
+
 def _zero(t, stream):
     import torch
     if stream is None:
@@ -534,7 +541,7 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, unit_offs
     sdx = cols if dx is None or dx.is_contiguous() else _row_stride(dx, "dx")
     rows = x.numel() // cols if cols else 0
     per, sw, wcode = _norm_weights(x, weight, None)
-    L, sdw, ws_bytes = lib(), 0, 0
+    L, sdw, ws_bytes = lib(), 0, 0 if workspace is None else _given(workspace)
     if dweight is not None or dbias is not None:
         gper, sdw, gcode = _norm_weights(x, dweight, dbias)
         if weight is not None and (gper != per or gcode != wcode):
@@ -547,7 +554,7 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, unit_offs
     _here(x, dy, weight, dx, dweight, dbias, workspace)
     _statistics(rows, x.get_device(), mean, rstd)
     status = L.hilberta_layer_norm_backward(dy.data_ptr(), x.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(), _ptr(dx),
-                                            _ptr(dweight), _ptr(dbias), _ptr(workspace), 0 if workspace is None else ws_bytes or workspace.nbytes,
+                                            _ptr(dweight), _ptr(dbias), _ptr(workspace), ws_bytes,
                                             rows, cols, per, sdy, sx, sdx, sw, sdw, _dtype_code(x), wcode, 1 if unit_offset else 0,
                                             _stream_ptr(stream))
     if status:
@@ -692,13 +699,15 @@ def packed_backward(dout, q, k, v, out, lse, dq, dk, dv, cu_seqlens, causal=True
     (taken from torch's allocator) or a uint8 tensor of packed_workspace() bytes."""
     if lse is None:
         raise ValueError("lse of the forward pass is needed")
+    ws_bytes = 0 if workspace is None else _given(workspace)
     T, H, Hk, D, st = _packed_args((dout, q, out, dq), (k, v, dk, dv), lse, cu_seqlens)
     if workspace is None:
-        workspace = _scratch(lib().hilberta_packed_workspace(T, H), q, stream)
+        ws_bytes = lib().hilberta_packed_workspace(T, H)
+        workspace = _scratch(ws_bytes, q, stream)
     else:
         _here(workspace)
     status = lib().hilberta_packed_backward(dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
-                                            dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+                                            dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), workspace.data_ptr(), ws_bytes,
                                             cu_seqlens.data_ptr(), cu_seqlens.numel() - 1, T, H, Hk, D, _dtype_code(q),
                                             _I64x16(st[0], st[1], st[3], st[4], st[12], st[13], st[15], st[16], st[6], st[7],
                                                     st[9], st[10], st[18], st[19], st[21], st[22]), 1 if causal else 0, scale, _stream_ptr(stream))

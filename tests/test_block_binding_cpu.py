@@ -19,3 +19,14 @@ def test_one_row_of_weights_has_any_stride():
                  (torch.zeros((1, 8)), torch.zeros(8)), (torch.zeros((1, 8)), torch.zeros((1, 8)).bfloat16())):
         with pytest.raises(ValueError):
             hb._norm_weights(x if a.dim() == 1 or a.shape[0] == 1 else torch.zeros((2, 3, 8)), a, b)
+
+
+def test_a_workspace_is_one_run_of_bytes():
+    """Every other byte of a buffer has the right count, but the library would write the bytes between them too."""
+    holes = torch.zeros(1 << 16, dtype=torch.uint8)[::2]
+    x, st = torch.zeros((4, 8)), torch.zeros(4)
+    with pytest.raises(ValueError, match="workspace"):
+        hb.layer_norm_backward(x, x, None, st, st, x.clone(), torch.zeros(8), None, workspace=holes)
+    q, lse, cu = torch.zeros((4, 1, 64)).bfloat16(), torch.zeros((1, 4)), torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="workspace"):
+        hb.packed_backward(q, q, q, q, q, lse, q.clone(), q.clone(), q.clone(), cu, workspace=holes)
