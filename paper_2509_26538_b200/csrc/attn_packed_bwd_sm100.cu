@@ -526,8 +526,8 @@ packed_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 const int tok = w.tok0 + (MODE == MODE_DQ ? r >> g_shift : r);   // the query's (DQ) or the key's (DKV) token
                 if (MODE == MODE_DQ && tok < w.len) {
                     const long long at = (long long)(w.row0 + tok) * prm.heads + w.head0 + (r & ((1 << g_shift) - 1));
-                    row_l2 = __ldg(prm.lse2 + at);
-                    row_dl = __ldg(prm.delta + at);
+                    row_l2 = prm.lse2[at];   // plain loads: the kernel before this one writes them while this one starts
+                    row_dl = prm.delta[at];
                 }
                 for (int rep = 0; ok && rep < (MODE == MODE_DKV ? prm.k_odd : 1); ++rep) {
                     for (int j = 0; j < w.count; ++j, ++g) {
