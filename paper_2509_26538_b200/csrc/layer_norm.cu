@@ -900,32 +900,44 @@ int launch_lanes(BackwardCall &c) {
     return HILBERTA_OK;
 }
 
+// The kernels that backward_shape() asks for at some width, type or alignment; no others are built.  (bf16 in vectors of four: what
+// vectors of eight leave out.)
+template <class T>
+constexpr bool reached(int vec, int each, int r) {
+    const bool bf16 = sizeof(T) == 2;
+    if (each % vec || (each == 4 && vec > 1) || (bf16 && vec == 4 && each % 8 == 0)) return false;
+    switch (each) {
+        case 4: return r == 4;
+        case 8: return r > 1 || !bf16;
+        case 12: return r <= 2;
+        case 16: return r == 1 || (r == 2 && bf16);
+    }
+    return r == 1;
+}
+
 template <class T, class W, int VEC, int EACH>
 int backward_by_rows(BackwardCall &c) {
-    constexpr int NV = EACH / VEC;
-    if constexpr (EACH <= 8)
-        if (c.g.r == 4) return launch_backward<T, W, VEC, NV, 4>(c);
-    if constexpr (EACH <= 16)
-        if (c.g.r == 2) return launch_backward<T, W, VEC, NV, 2>(c);
-    return launch_backward<T, W, VEC, NV, 1>(c);
+    if constexpr (reached<T>(VEC, EACH, 4))
+        if (c.g.r == 4) return launch_backward<T, W, VEC, EACH / VEC, 4>(c);
+    if constexpr (reached<T>(VEC, EACH, 2))
+        if (c.g.r == 2) return launch_backward<T, W, VEC, EACH / VEC, 2>(c);
+    if constexpr (reached<T>(VEC, EACH, 1))
+        if (c.g.r == 1) return launch_backward<T, W, VEC, EACH / VEC, 1>(c);
+    return HILBERTA_ERR_UNSUPPORTED;
 }
 
 template <class T, class W, int VEC>
 int backward_by_each(BackwardCall &c) {
     switch (c.g.each) {
+        case 4: return backward_by_rows<T, W, VEC, 4>(c);
         case 8: return backward_by_rows<T, W, VEC, 8>(c);
+        case 12: return backward_by_rows<T, W, VEC, 12>(c);
         case 16: return backward_by_rows<T, W, VEC, 16>(c);
+        case 20: return backward_by_rows<T, W, VEC, 20>(c);
         case 24: return backward_by_rows<T, W, VEC, 24>(c);
+        case 28: return backward_by_rows<T, W, VEC, 28>(c);
         case 32: return backward_by_rows<T, W, VEC, 32>(c);
-    }
-    if constexpr (VEC <= 4) {
-        switch (c.g.each) {
-            case 4: return backward_by_rows<T, W, VEC, 4>(c);
-            case 12: return backward_by_rows<T, W, VEC, 12>(c);
-            case 20: return backward_by_rows<T, W, VEC, 20>(c);
-            case 28: return backward_by_rows<T, W, VEC, 28>(c);
-            case 36: return backward_by_rows<T, W, VEC, 36>(c);
-        }
+        case 36: return backward_by_rows<T, W, VEC, 36>(c);
     }
     return HILBERTA_ERR_UNSUPPORTED;
 }
