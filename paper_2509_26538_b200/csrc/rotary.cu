@@ -97,6 +97,13 @@ struct Chunk {   // 16 bytes
             }
         }
     }
+    // elements 2 i and 2 i + 1 as `from` has them, bit for bit (a NaN does not survive the way through fp32)
+    __device__ __forceinline__ void copy_pair(int i, const Chunk &from) {
+        uint32_t *w = &v.x;
+        const uint32_t *o = &from.v.x;
+        if constexpr (sizeof(T) == 4) w[2 * i] = o[2 * i], w[2 * i + 1] = o[2 * i + 1];
+        else w[i] = o[i];
+    }
 };
 
 // The frequencies, from the parameters (where lanes that want different ones are served one after the other) to shared
@@ -211,12 +218,10 @@ rotary_kernel(const __grid_constant__ Params p, const Divider per_batch, const D
 #pragma unroll
                 for (int e = 0; e < N / 2; ++e) {
                     const float x0 = a[i].get(2 * e), y0 = a[i].get(2 * e + 1), x1 = b[i].get(2 * e), y1 = b[i].get(2 * e + 1);
-                    // elements behind the rotated part stay, whatever they hold
-                    const bool r0 = j0 + e < p.pairs, r1 = j0 + N / 2 + e < p.pairs;
-                    fa[2 * e] = r0 ? turned(x0, y0, cs[e], -sn[e]) : x0;
-                    fa[2 * e + 1] = r0 ? turned(y0, x0, cs[e], sn[e]) : y0;
-                    fb[2 * e] = r1 ? turned(x1, y1, cs[N / 2 + e], -sn[N / 2 + e]) : x1;
-                    fb[2 * e + 1] = r1 ? turned(y1, x1, cs[N / 2 + e], sn[N / 2 + e]) : y1;
+                    fa[2 * e] = turned(x0, y0, cs[e], -sn[e]);
+                    fa[2 * e + 1] = turned(y0, x0, cs[e], sn[e]);
+                    fb[2 * e] = turned(x1, y1, cs[N / 2 + e], -sn[N / 2 + e]);
+                    fb[2 * e + 1] = turned(y1, x1, cs[N / 2 + e], sn[N / 2 + e]);
                 }
             } else {
 #pragma unroll
@@ -227,11 +232,18 @@ rotary_kernel(const __grid_constant__ Params p, const Divider per_batch, const D
                 }
             }
             T *row = (T *)p.out + at.out + (h + i) * p.oh;
+            // interleaved: elements behind the rotated part stay, whatever they hold
             Chunk<T> o;
             o.set(fa);
+#pragma unroll
+            for (int e = 0; INTERLEAVED && e < N / 2; ++e)
+                if (j0 + e >= p.pairs) o.copy_pair(e, a[i]);
             __stcs(reinterpret_cast<uint4 *>(row + ca), o.v);
             if (!INTERLEAVED || cb < p.dim) {
                 o.set(fb);
+#pragma unroll
+                for (int e = 0; INTERLEAVED && e < N / 2; ++e)
+                    if (j0 + N / 2 + e >= p.pairs) o.copy_pair(e, b[i]);
                 __stcs(reinterpret_cast<uint4 *>(row + cb), o.v);
             }
         }
@@ -294,6 +306,9 @@ rotary_shifted_kernel(const __grid_constant__ Params p, const Divider per_batch,
             f[i] = c0 + i < 2 * p.pairs ? turned(x, (float)row[partner[i]], cs[i], sn[i]) : x;
         }
         o.set(f);
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i)
+            if (c0 + 2 * i >= 2 * p.pairs) o.copy_pair(i, a);
         *reinterpret_cast<uint4 *>((T *)p.out + at.out + h * p.oh + c0) = o.v;
     }
 }
