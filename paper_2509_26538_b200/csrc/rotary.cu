@@ -49,7 +49,7 @@ __device__ __forceinline__ int remainder_of(int pos, unsigned long long turns, u
     return (int)(u - (quarter << 30));
 }
 
-// cos and sin of two angles by their Taylor series, |angle| <= pi / 4: the first terms left out are below 2^-32 and 2^-29 of
+// cos and sin of two angles by their Taylor series, |angle| <= pi / 4: the first terms left out are below 2^-32 and 2^-28 of
 // the result.  Packed arithmetic: two angles an instruction (the library's sincospif for each, 3.2 million angles and no more
 // than one head to use them, took 14.5 us in all).
 __device__ __forceinline__ void cos_sin2(const int *pos, const unsigned long long *turns, float2 &cos, float2 &sin) {
