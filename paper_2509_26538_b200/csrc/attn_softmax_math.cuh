@@ -24,11 +24,15 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // x = n + f with n = round(x) (adding 1.5 * 2^23 leaves the integer in the low mantissa
 // bits), f in [-0.5, 0.5]; 2^f by a cubic (max relative error 7.8e-5, far below bf16
 // rounding), 2^n by an exponent add.  Used for a fixed share of the exponentials so that
-// the MUFU unit and the FMA pipes split the work.  x is clamped at -126 (result ~0).
+// the MUFU unit and the FMA pipes split the work.  x is clamped at -126 (result ~0); with degree 4 just above -127, where f is
+// 2^-17, the polynomial 1 + 4.5e-6 and the exponent's field 0: what is left is 5e-44, and nothing in bf16.  A key that a mask
+// hides has a weight of zero then, however large its value; 2^-126 of 3e38 is 3.5.
+template <int DEG>
+constexpr float EX2_LEAST = DEG == 4 ? -126.99999237060547f : -126.f;
 template <int DEG = 3>
 __device__ __forceinline__ float2 ex2_poly2(float2 x) {
-    x.x = fmaxf(x.x, -126.f);
-    x.y = fmaxf(x.y, -126.f);
+    x.x = fmaxf(x.x, EX2_LEAST<DEG>);
+    x.y = fmaxf(x.y, EX2_LEAST<DEG>);
     const float2 t = __fadd2_rn(x, make_float2(12582912.f, 12582912.f));
     const float2 n = __fadd2_rn(t, make_float2(-12582912.f, -12582912.f));
     const float2 f = __fadd2_rn(x, make_float2(-n.x, -n.y));
@@ -55,7 +59,7 @@ __device__ __forceinline__ float2 ex2_poly2(float2 x) {
 // same bits.
 template <int DEG = 3>
 __device__ __forceinline__ float ex2_poly1(float x) {
-    x = fmaxf(x, -126.f);
+    x = fmaxf(x, EX2_LEAST<DEG>);
     const float t = __fadd_rn(x, 12582912.f);
     const float n = __fadd_rn(t, -12582912.f);
     const float f = __fadd_rn(x, -n);
