@@ -916,8 +916,11 @@ extern "C" int hilberta_packed_backward(const void *dout, const void *q, const v
     const int k_heads = p.group / p.splits, gk = packed::packed_heads(k_heads);
     p.k_shift = __builtin_ctz((unsigned)gk);
     p.k_odd = k_heads / gk;
+    auto units = [&](int per, int parts) { return (unsigned)(((long long)total / per + std::min(n_seq, total)) * parts); };   // at most
+    p.dkv_units = units(BM, kv_heads * p.splits);
+    const unsigned ctas = p.dkv_units + units(per_tile, kv_heads * p.odd);
     // blocks of the longest unit there may be: keys of a query tile, or queries of the heads of a key tile
-    p.unit_wait = packed::unit_wait((((long long)total << p.k_shift) + BK - 1) / BK * p.k_odd);
+    p.unit_wait = packed::unit_wait((((long long)total << p.k_shift) + BK - 1) / BK * p.k_odd, ctas, sms);
     p.partial = p.splits > 1 ? (float *)((char *)workspace + statistics_bytes(total, heads)) : nullptr;
     CUtensorMap mq, mk, mv, mdo, mqs, mdos;
     if ((rc = packed::make_map(&mdo, dout, total, heads, head_dim, strides[0], strides[1], g, per_tile)) != HILBERTA_OK) return rc;
@@ -939,9 +942,6 @@ extern "C" int hilberta_packed_backward(const void *dout, const void *q, const v
                                (const __nv_bfloat16 *)dout, (const __nv_bfloat16 *)out, lse, lse2, delta, total, Divider(heads), (long long)strides[0],
                                (long long)strides[1], (long long)strides[8], (long long)strides[9]));
     HB_LAUNCHED();
-    auto units = [&](int per, int parts) { return (unsigned)(((long long)total / per + std::min(n_seq, total)) * parts); };   // at most
-    p.dkv_units = units(BM, kv_heads * p.splits);
-    const unsigned ctas = p.dkv_units + units(per_tile, kv_heads * p.odd);
     HB_CUDA(launch_overlapping(head_dim == 128 ? packed_bwd_kernel<128> : packed_bwd_kernel<64>, ctas, THREADS, (size_t)SMEM_BYTES, 1, st,
                                true, mq, mk, mv, mdo, mqs, mdos, p));
     HB_LAUNCHED();

@@ -704,13 +704,13 @@ extern "C" int hilberta_packed_forward(const void *q, const void *k, const void 
     p.lse = lse;
     const float s = scale > 0.f ? scale : 1.f / sqrtf((float)head_dim);
     p.scale_log2 = s * 1.4426950408889634f;
-    p.unit_wait = packed::unit_wait(((long long)total + BN - 1) / BN);
+    const unsigned ctas = (unsigned)units(p.tiles);
+    p.unit_wait = packed::unit_wait(((long long)total + BN - 1) / BN, ctas, sms);
     CUtensorMap mq, mk, mv, mo;
     if ((rc = packed::make_map(&mq, q, total, heads, head_dim, strides[0], strides[1], g, per_tile)) != HILBERTA_OK) return rc;
     if ((rc = packed::make_map(&mk, k, total, kv_heads, head_dim, strides[2], strides[3], 1, BN)) != HILBERTA_OK) return rc;
     if ((rc = packed::make_map(&mv, v, total, kv_heads, head_dim, strides[4], strides[5], 1, BN)) != HILBERTA_OK) return rc;
     if ((rc = packed::make_map(&mo, out, total, heads, head_dim, strides[6], strides[7], g, 32 / g)) != HILBERTA_OK) return rc;
-    const unsigned ctas = (unsigned)units(p.tiles);
     const bool overlap = (size_t)total * heads * head_dim * 2 <= kOverlapBytes / 4;
     HB_CUDA(launch_overlapping(head_dim == 128 ? packed_kernel<128> : packed_kernel<64>, ctas, THREADS, (size_t)smem_bytes(head_dim), 1,
                                (cudaStream_t)stream, overlap, mq, mk, mv, mo, p));

@@ -149,8 +149,9 @@ int backward_status(bool *expired);
 
 // Deadline of waits that last a whole unit -- for the next unit, or for the end of this one in a role with little to do -- where the
 // others last a block.  A unit of up to `blocks` streamed blocks takes some 4000 cycles for each: four times that, behind the
-// usual second.  (64 heads to a key head and 2^20 tokens: 524288 blocks in a unit, more than a second.)
-inline long long unit_wait(long long blocks) { return ptx::WAIT_CYCLES + 16384 * blocks; }
+// usual second.  (64 heads to a key head and 2^20 tokens: 524288 blocks in a unit, more than a second.)  Nor is there a next unit
+// at once where many sequences are empty: an SM asks for its share of the launch's `ctas` one after the other, some 900 cycles each.
+inline long long unit_wait(long long blocks, long long ctas, int sms) { return ptx::WAIT_CYCLES + 16384 * (blocks + ctas / sms); }
 
 // The largest power of two that divides the heads of a group, at most 16: so many heads of one token are rows of a
 // query tile next to one another.

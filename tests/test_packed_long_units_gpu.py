@@ -48,3 +48,28 @@ def test_a_unit_of_more_than_a_second():
         assert ((got.float() - ref.float()).abs() <= 2.0 ** -7 * ref.float().abs() + 1e-4 * size).all()
     del q, dout, out, lse, dq
     torch.cuda.empty_cache()
+
+
+def test_more_than_a_second_without_a_unit():
+    """65536 sequences, all empty but the last: 396 million units that are not there, one after the other."""
+    T, H, D = 65536, 6000, 64
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("needs 80 GB of device memory")
+    step = 8 * H + D
+    line = torch.randn(T * step + 128, generator=torch.Generator(device="cuda").manual_seed(61), device="cuda", dtype=torch.bfloat16)
+    q, k, v = (line.as_strided((T, H, D), (step, 8, 1), 64 * i) for i in range(3))
+    out = torch.full((T, H, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    # one token at the very end: its output is its value
+    cu = torch.full((65537,), T - 1, dtype=torch.int32, device="cuda")
+    cu[-1] = T
+    start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    start.record()
+    hb.packed_forward(q, k, v, out, cu)
+    end.record()
+    assert hb.packed_status() == 0
+    print("ms:", start.elapsed_time(end))
+    assert start.elapsed_time(end) > 1000   # else this is no test
+    assert torch.equal(out[-1], v[-1])
+    assert (out[:-1] == 7.0).all()
+    del line, q, k, v, out
+    torch.cuda.empty_cache()
