@@ -356,9 +356,10 @@ int hilberta_forward_host(const void *q, const void *k, const void *v, void *out
  *   weight, bias    device pointers or NULL (1 and 0): row r uses row r / rows_per_group of each, rows stride_w
  *                   elements apart (two slices of one modulation tensor share it); rows_per_group = 0: one row
  *                   for all.  unit_offset != 0 adds 1 to the weight.
+ *                   x and y may be slices of one buffer, side by side (same stride).
  *   mean, rstd      device pointers to [rows] fp32 or NULL: what the backward pass reads.
- *   rows >= 0; 1 <= cols <= 16384 (more: ERR_UNSUPPORTED); any stride and alignment (16-byte aligned rows are
- *   faster); eps >= 0.
+ *   rows >= 0; 1 <= cols <= 16384 (more: ERR_UNSUPPORTED); any stride and alignment (faster with 16-byte aligned rows of
+ *   a multiple of 8 columns; forward in fp32, of 4); eps >= 0.
  *   dtype           HILBERTA_BF16 or HILBERTA_FP32; weight_dtype the same or HILBERTA_FP32.  Sums are fp32.
  * Errors: ERR_INVALID, ERR_UNSUPPORTED, ERR_ARCH, ERR_CUDA. */
 int hilberta_layer_norm(const void *x, const void *weight, const void *bias, void *y, float *mean, float *rstd,
@@ -368,7 +369,8 @@ int hilberta_layer_norm(const void *x, const void *weight, const void *bias, voi
 /* Gradients of sum(y * dy):  with n = (x - mean) * rstd and g = dy * (weight [+ 1]),
  *     dx = rstd * (g - sum g / cols - n * sum(g n) / cols),   dweight = sum_rows dy n,   dbias = sum_rows dy,
  * the latter two over the rows of each group (rows stride_dw elements apart, weight_dtype).
- *   dx, dweight, dbias   any of them may be NULL, not all three.  dx may be dy or x itself (same stride).
+ *   dx, dweight, dbias   any of them may be NULL, not all three.  dx may be dy or x itself, or lie beside them in one
+ *                        buffer (same stride).
  *   mean, rstd           as hilberta_layer_norm wrote them.
  *   workspace            hilberta_layer_norm_workspace() bytes of device memory, 16-byte aligned, which the call
  *                        overwrites (NULL where that says 0, or without dweight and dbias); calls that may overlap on the device
@@ -440,9 +442,14 @@ int hilberta_rotary_frequencies(double *inv_freq, int pairs, double base, int sc
  *   cu_seqlens    DEVICE pointer to n_seq + 1 ascending int32, from >= 0 to <= total.  Sequences may be empty.  Rows
  *                 outside all sequences are neither read into a result nor written, whatever they hold.  Values that
  *                 are not ascending or leave [0, total] give undefined results and no access out of range.
- *   kv_heads divides heads; head_dim 64 or 128; dtype HILBERTA_BF16 (others: ERR_UNSUPPORTED); n_seq <= 65536.
+ *   kv_heads divides heads; head_dim 64 or 128; dtype HILBERTA_BF16 (others: ERR_UNSUPPORTED); n_seq <= 65536;
+ *   total <= 2^26, heads <= 65536, total * heads <= 2^31 - 2^24 (more: ERR_UNSUPPORTED).  Work is found by reading
+ *   cu_seqlens, which beyond some thousand short sequences takes longer than the attention itself.
  *   scale         <= 0 selects 1 / sqrt(head_dim).
- *   values        those of one sequence must be finite for it; other sequences do not matter to it.
+ *   values        those of one sequence must be finite for it; other sequences do not matter to it: its results have
+ *                 the same bits whatever they hold.  A key that a token does not see leaves no trace of its value.
+ *   precision     scores, sums and lse are fp32; the weights are rounded to bf16 before they meet v, as the tensor
+ *                 cores take them.  out is off by 2.0e-3 of its norm (its own rounding alone: 1.7e-3), lse by 1e-7.
  * Errors: ERR_INVALID, ERR_UNSUPPORTED, ERR_ARCH, ERR_CUDA. */
 int hilberta_packed_forward(const void *q, const void *k, const void *v, void *out, float *lse, const int32_t *cu_seqlens,
                             int n_seq, int total, int heads, int kv_heads, int head_dim, int dtype, const int64_t *strides,
@@ -457,7 +464,9 @@ int hilberta_packed_forward(const void *q, const void *k, const void *v, void *o
  *                 overwrites; calls that may overlap on the device need one each.  ERR_BUFFER if it is too small.
  *                 The bytes are those for the current device: two floats a row and head, and up to 160 MB of partial
  *                 sums where `total` is small next to the device.
- * Every sum is taken in a fixed order: the same call gives the same bits. */
+ * Sums are fp32; P and dS are rounded to bf16 before the products that sum over them, and sum_d dout * out is taken from
+ * the rounded `out` for sequences of more than 128 tokens: gradients are off by 2.4e-3 to 2.9e-3 of their norm, where
+ * rounding the results alone costs 1.7e-3.  Every sum is taken in a fixed order: the same call gives the same bits. */
 int hilberta_packed_backward(const void *dout, const void *q, const void *k, const void *v, const void *out, const float *lse,
                              void *dq, void *dk, void *dv, void *workspace, size_t workspace_bytes, const int32_t *cu_seqlens,
                              int n_seq, int total, int heads, int kv_heads, int head_dim, int dtype, const int64_t *strides,

@@ -13,6 +13,9 @@
 // feels most, its dS being a small difference; there all keys of a row are in one block, and the element-wise step takes
 // delta = sum_j P_ij dP_ij itself.  (Error of dq against 64 bits, sequences of 2 ... 5 tokens 4.6e-3 and 2.5e-3 of the
 // norm, 64 ... 77 tokens 3.1e-3 and 2.4e-3, 300 tokens 2.9e-3 and 2.5e-3.)
+// P and dS are rounded to bf16 before the products over queries or keys, as the tensor cores take them; each in two parts, which
+// would keep 16 bits, takes three products more than these seven.  (Gradients off by 2.4e-3 ... 2.9e-3 of their norm; rounding
+// the results alone: 1.7e-3.)
 // Bound by the chain dP -> phase 2 -> output products -> next dP: 2.1 us a block in DKV mode (four products, 1.5 at the matrix
 // rate of a large library product), 1.4 in DQ mode (three, 1.1); tensor pipe 61 % of the cycles.  Measured (B200, us): four
 // documents of 333 ... 4096 tokens, 16 heads over 4 key heads, causal, head dim 128: 300 (statistics 15 of it), with each mode's

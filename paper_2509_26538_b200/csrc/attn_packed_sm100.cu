@@ -16,10 +16,12 @@
 //
 // Bound by the chain scores -> softmax -> P V of its two tiles, like the sparse forward kernel whose loop this is: 2.0 us for
 // 128 keys of two tiles at head dim 128, 1.5 at the matrix rate of a large library product.  Measured (B200, us; TFLOP/s of
-// the pairs that count): 4608 tokens of 24 heads 218 (1195), causal 128 (1020); four documents of 1911 ... 4096 tokens, 32
-// heads over 8 key heads, causal 304 (1075).  What it took: the unit kept in shared memory and not in registers beside 128
+// the pairs that count): 4608 tokens of 24 heads 216 (1210), causal 121 (1080); four documents of 1911 ... 4096 tokens, 32
+// heads over 8 key heads, causal 297 (1100).  What it took: the unit kept in shared memory and not in registers beside 128
 // scores 530 -> 316 (documents, spills); sequences by length 765 -> 382 (images of three sizes); bulk stores 316 -> 296.
-// A handful of prompts is latency: 7.5 us for ten of 1 ... 77 tokens, of which the launch, finding the unit and one block.
+// A handful of prompts is latency: 8 us for ten of 1 ... 77 tokens, of which the launch, finding the unit and one block.
+// Weights are rounded to bf16 before they meet V, as the tensor cores take them: out is off by 2.0e-3 of its norm (1.7e-3 by its
+// own rounding); the row sum has them in fp32.
 #include <algorithm>
 #include <mutex>
 

@@ -8,10 +8,10 @@
 // once.  A row stays in registers between its statistics and its output; sums are fp32, the variance is taken
 // around the mean that has already been summed (no difference of large squares).
 // Measured (B200, us; share of the copy bandwidth).  Forward: 33792 x 1536 bf16, modulated 40 (79 %), 40000 x 1024 bf16 29 (85 %),
-// 12000 x 4096 fp32 64 (94 %): what is left in bf16 is unpacking and packing on the integer pipe, half busy.  Backward: 40000 x
-// 1024 bf16 46 (82 %), 36864 x 1152 bf16 54 (73 %), 12000 x 4096 fp32 97 (93 %), 3000 x 16000 bf16 97 (45 %: a row at a time, 15
-// warps and one barrier a row), of which 5 ... 7 add the CTAs' sums up; rows that are not aligned take elements one by one (30000 x
-// 1001 bf16 forward 48, backward 67: 38 and 41 %).
+// 12000 x 4096 fp32 63 (95 %): what is left in bf16 is unpacking and packing on the integer pipe, half busy.  Backward: 40000 x
+// 1024 bf16 46 (82 %), 36864 x 1152 bf16 52 (75 %), 12000 x 4096 fp32 97 (93 %), 3000 x 16000 bf16 96 (46 %: a row at a time, 15
+// warps and one barrier a row), of which 5 ... 7 add the CTAs' sums up; rows that are not aligned, or whose columns are no multiple of
+// a vector (of eight backward, whatever the type), take elements one by one (30000 x 1001 bf16 forward 47, backward 66: 39 and 42 %).
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -443,8 +443,8 @@ layer_norm_bwd_kernel(const BackwardParams prm) {
     float2 dw[P] = {}, db[P] = {}, w[KEEP_W ? P : (VEC > 1 ? VEC / 2 : 1)];
     // This thread's vector v: its column, and whether there is one.  A warp's vectors lie side by side, at distances that the
     // compiler knows (up to 36 registers otherwise, whose spills come back from L2: 3000 x 10001 bf16 250 us, 83 so; 12000 x
-    // 4096 fp32 102 and 97; 30000 x 1001 bf16 79 and 67), but the team's where few vectors are of 8 bytes or single fp32 elements
-    // (36864 x 1152 bf16 79 us with a warp's side by side, 54 so; 3 x 1777 x 777 fp32 20 and 17.7).
+    // 4096 fp32 102 and 97; 30000 x 1001 bf16 79 and 66), but the team's where few vectors are of 8 bytes or single fp32 elements
+    // (36864 x 1152 bf16 79 us with a warp's side by side, 52 so; 3 x 1777 x 777 fp32 20 and 17.7).
     constexpr bool NEAR = !KEEP_W || VEC * sizeof(T) >= 16 || VEC * sizeof(T) == 2;
     const int apart = NEAR ? 32 * VEC : threads * VEC;
     const int col0 = (NEAR ? tid / 32 * NV * 32 + lane : tid) * VEC, after = cols - col0;

@@ -9,8 +9,8 @@
 // fraction; the product with the position wraps where the angle does), once per token and pair for all the heads
 // of a thread.  Only the remainder, at most an eighth of a turn, becomes fp32.
 // Measured (B200, us; share of the copy bandwidth): 12 heads of 16384 tokens fp32 33 (93 %), 24 heads bf16 34 (90 %), with
-// the entry gather and three axes 41 (77 %: rows of 256 bytes in Hilbert order); one head has the angles to itself, 100000
-// tokens 8.5 (47 %); 16 single tokens of 32 heads 1.8, a launch.
+// the entry gather and three axes 40 (79 %: rows of 256 bytes in Hilbert order); one head has the angles to itself, 100000
+// tokens 9.4 (42 %); 16 single tokens of 32 heads 2, a launch.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -255,7 +255,7 @@ rotary_kernel(const __grid_constant__ Params p, const Divider per_batch, const D
 
 // Half layout with a pair count that leaves the second half unaligned: a thread has 16 bytes of the output of
 // heads_per_thread heads and reads the elements they are paired with one by one.  Not in place: those belong to other
-// threads.  (8 heads of 16384 tokens, head dim 128, 33 pairs, bf16: 53 us with a pair a thread, 20 so.)
+// threads.  (8 heads of 16384 tokens, head dim 128, 33 pairs, bf16: 53 us with a pair a thread, 17 so.)
 template <class T>
 __global__ void __launch_bounds__(THREADS)
 rotary_shifted_kernel(const __grid_constant__ Params p, const Divider per_batch, const Divider per_row) {
